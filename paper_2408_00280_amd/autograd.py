@@ -9,12 +9,19 @@ the backward returns no gradient for the hyper-parameters.
 Inputs are time-major, ``x[T, ...]``, float32 or bfloat16; the output is the spike train
 ``y[T, ...]`` as 0/1 values of the same dtype.  The arithmetic runs in the HIP kernels;
 torch allocates and orders the work on its current stream.
+
+Beside the LIF layers stand the sequence operators that join them in one block, on the same
+[T, B, F] data: causal_conv / CausalConv, selective_scan / SelectiveScan and block_norm /
+BlockNorm.
 """
 from __future__ import annotations
 
-import torch
+import math
 
-from . import layer
+import torch
+from torch.autograd.function import once_differentiable
+
+from . import layer, sequence
 
 _IO = {torch.float32: "f32", torch.bfloat16: "bf16"}
 
@@ -168,3 +175,172 @@ class LIFStack(torch.nn.Module):
     def extra_repr(self) -> str:
         return (f"layers={self.gains.shape[0] + 1}, features={self.gains.shape[1]}, decay={self.decay}, "
                 f"v_th={self.v_th}, v_reset={self.v_reset}, alpha={self.alpha}, reset={self.reset}")
+
+
+class FusedConv(torch.autograd.Function):
+    """sequence.conv_forward / conv_backward; the outputs are y and the last W-1 inputs."""
+
+    @staticmethod
+    def forward(ctx, x, weight, bias, state, lengths, act, want_state):
+        W = weight.shape[1]
+        out = torch.empty((W - 1, *x.shape[1:]), dtype=x.dtype, device=x.device) if want_state else None
+        y = sequence.conv_forward(x, weight, bias, act=act, state=state, state_out=out, lengths=lengths)
+        ctx.save_for_backward(x, weight, bias, state, lengths)
+        ctx.act = act
+        ctx.set_materialize_grads(False)
+        return y, out
+
+    @staticmethod
+    @once_differentiable
+    def backward(ctx, grad_y, grad_state_out):
+        x, weight, bias, state, lengths = ctx.saved_tensors
+        grad_y = torch.zeros_like(x) if grad_y is None else grad_y
+        if grad_state_out is not None:
+            grad_state_out = grad_state_out.contiguous()
+        g = sequence.conv_backward(x, weight, bias, grad_y, act=ctx.act, state=state, lengths=lengths,
+                                   grad_state_out=grad_state_out)
+        return (*g, None, None, None)
+
+
+def causal_conv(x, weight, bias=None, *, act="silu", state=None, lengths=None, return_state=False):
+    """Short causal convolution of x[T, B, F] along time (see sequence.conv_forward), with
+    gradients for x, weight, bias and state.  Returns y, or (y, the last W-1 inputs)."""
+    y, out = FusedConv.apply(x, weight, bias, state, lengths, act, return_state)
+    return (y, out) if return_state else y
+
+
+class CausalConv(torch.nn.Module):
+    """Short causal convolution along the leading (time) axis, one filter per feature, with
+    bias and activation (None or "silu")."""
+
+    def __init__(self, features: int, width: int = 4, bias: bool = True, act: str | None = "silu"):
+        super().__init__()
+        bound = 1 / math.sqrt(width)
+        self.weight = torch.nn.Parameter(torch.empty(features, width).uniform_(-bound, bound))
+        self.bias = torch.nn.Parameter(torch.empty(features).uniform_(-bound, bound)) if bias else None
+        self.act = act
+
+    def _args(self):
+        return self.weight.float(), None if self.bias is None else self.bias.float()
+
+    def forward(self, x, *, state=None, lengths=None, return_state=False):
+        return causal_conv(x, *self._args(), act=self.act, state=state, lengths=lengths, return_state=return_state)
+
+    @torch.no_grad()
+    def step(self, x, state):
+        """One step x[B, F] on state[W-1, B, F], which is updated in place: y[B, F]."""
+        return sequence.conv_forward(x[None], *self._args(), act=self.act, state=state, state_out=state)[0]
+
+    def extra_repr(self) -> str:
+        return f"features={self.weight.shape[0]}, width={self.weight.shape[1]}, act={self.act}"
+
+
+class FusedScan(torch.autograd.Function):
+    """sequence.scan_forward / scan_backward; the outputs are y and the state after the last step."""
+
+    @staticmethod
+    def forward(ctx, x, dt, A, Bm, Cm, D, dt_bias, h_in, lengths, softplus, want_state):
+        out = torch.empty((x.shape[1], *A.shape), dtype=torch.float32, device=x.device) if want_state else None
+        y, saved = sequence.scan_forward(x, dt, A, Bm, Cm, D, dt_bias, softplus=softplus, h_in=h_in, h_out=out,
+                                         lengths=lengths, train=any(ctx.needs_input_grad))
+        ctx.save_for_backward(x, dt, A, Bm, Cm, D, dt_bias, h_in, lengths, saved)
+        ctx.softplus = softplus
+        ctx.set_materialize_grads(False)
+        return y, out
+
+    @staticmethod
+    @once_differentiable
+    def backward(ctx, grad_y, grad_h_out):
+        *args, h_in, lengths, saved = ctx.saved_tensors
+        grad_y = torch.zeros_like(args[0]) if grad_y is None else grad_y
+        if grad_h_out is not None:
+            grad_h_out = grad_h_out.contiguous()
+        g = sequence.scan_backward(*args, saved, grad_y, softplus=ctx.softplus, h_in=h_in, lengths=lengths,
+                                   grad_h_out=grad_h_out)
+        return (*g, None, None, None)
+
+
+def selective_scan(x, dt, A, Bm, Cm, D=None, dt_bias=None, *, softplus=True, h_in=None, lengths=None,
+                   return_state=False):
+    """Selective state space scan of x[T, B, F] (see sequence.scan_forward), with gradients for
+    every input.  Returns y, or (y, the state [B, F, S] after the last step)."""
+    y, out = FusedScan.apply(x, dt, A, Bm, Cm, D, dt_bias, h_in, lengths, softplus, return_state)
+    return (y, out) if return_state else y
+
+
+class SelectiveScan(torch.nn.Module):
+    """Selective state space scan along the leading (time) axis: rates A = -exp(A_log) [F, S],
+    skip weights D and step biases dt_bias [F]; x, dt [T, B, F] and B, C [T, B, G, S] are
+    inputs (projections of the block's input)."""
+
+    def __init__(self, features: int, states: int = 16, dt_min: float = 1e-3, dt_max: float = 0.1):
+        super().__init__()
+        rates = torch.arange(1, states + 1, dtype=torch.float32).expand(features, states)
+        self.A_log = torch.nn.Parameter(torch.log(rates))
+        self.D = torch.nn.Parameter(torch.ones(features))
+        dt = torch.exp(torch.empty(features).uniform_(math.log(dt_min), math.log(dt_max)))
+        self.dt_bias = torch.nn.Parameter(torch.log(torch.expm1(dt)))     # softplus(dt_bias) = dt
+
+    def _A(self):
+        return -torch.exp(self.A_log.float())
+
+    def forward(self, x, dt, Bm, Cm, *, h_in=None, lengths=None, return_state=False):
+        return selective_scan(x, dt, self._A(), Bm, Cm, self.D.float(), self.dt_bias.float(), h_in=h_in,
+                              lengths=lengths, return_state=return_state)
+
+    @torch.no_grad()
+    def step(self, x, dt, Bm, Cm, h):
+        """One step x, dt [B, F], Bm, Cm [B, G, S] on the state h[B, F, S], which is updated in
+        place: y[B, F]."""
+        y, _ = sequence.scan_forward(x[None], dt[None], self._A(), Bm[None], Cm[None], self.D.float(),
+                                     self.dt_bias.float(), h_in=h, h_out=h)
+        return y[0]
+
+    def extra_repr(self) -> str:
+        return f"features={self.A_log.shape[0]}, states={self.A_log.shape[1]}"
+
+
+class FusedBlockNorm(torch.autograd.Function):
+    """sequence.norm_forward / norm_backward."""
+
+    @staticmethod
+    def forward(ctx, y, r, z, w_post, scale, w_pre, lengths, eps):
+        r_new, u, rstd = sequence.norm_forward(y, r, z, w_post, scale, w_pre, eps=eps, lengths=lengths,
+                                               train=any(ctx.needs_input_grad))
+        ctx.save_for_backward(y, r, z, w_post, scale, w_pre, rstd, lengths)
+        ctx.eps = eps
+        ctx.set_materialize_grads(False)
+        return r_new, u
+
+    @staticmethod
+    @once_differentiable
+    def backward(ctx, grad_r_new, grad_u):
+        *args, lengths = ctx.saved_tensors
+        return (*sequence.norm_backward(*args, grad_r_new, grad_u, eps=ctx.eps, lengths=lengths), None, None)
+
+
+def block_norm(y, r=None, z=None, w_post=None, scale=None, w_pre=None, *, eps=1e-5, lengths=None):
+    """A block's gate, norm and scaled residual with the next block's norm (see
+    sequence.norm_forward), with gradients for every input: (r_new, u or None)."""
+    return FusedBlockNorm.apply(y, r, z, w_post, scale, w_pre, lengths, eps)
+
+
+class BlockNorm(torch.nn.Module):
+    """The end of a block and the start of the next: r_new = r + scale * norm(y * silu(z)) and
+    u = norm(r_new), with learned weights for both norms and the scale (each can be left out)."""
+
+    def __init__(self, features: int, *, post: bool = True, scale: float | None = 1.0, pre: bool = True,
+                 eps: float = 1e-5):
+        super().__init__()
+        self.w_post = torch.nn.Parameter(torch.ones(features)) if post else None
+        self.scale = torch.nn.Parameter(torch.full((features,), float(scale))) if scale is not None else None
+        self.w_pre = torch.nn.Parameter(torch.ones(features)) if pre else None
+        self.features, self.eps = features, eps
+
+    def forward(self, y, r=None, z=None, *, lengths=None):
+        w = (None if p is None else p.float() for p in (self.w_post, self.scale, self.w_pre))
+        return block_norm(y, r, z, *w, eps=self.eps, lengths=lengths)
+
+    def extra_repr(self) -> str:
+        parts = [n for n in ("w_post", "scale", "w_pre") if getattr(self, n) is not None]
+        return f"features={self.features}, {', '.join(parts)}, eps={self.eps}"

@@ -2,8 +2,8 @@
 
 The kernel variants are split over several translation units (one per forward I/O dtype and
 spike format, one per backward I/O dtype, the same for the gain-fed layer and for the
-stack fused across depth, the gain kernels, the serial baseline, the C ABI) that compile in
-parallel and link into one shared library.
+stack fused across depth, the gain kernels, the serial baseline, the sequence operators, the
+C ABI) that compile in parallel and link into one shared library.
 """
 from __future__ import annotations
 
@@ -38,6 +38,8 @@ UNITS = (
        for io in (0, 1) for spk in (0, 1, 2)]
     + [(f"stackb_io{io}", "lif_stack.hip", [f"-DSNNLIF_IO={io}", "-DSNNLIF_STACK_BWD=1"]) for io in (0, 1)]
     + [("glue", "lif_glue.hip", []), ("serial", "lif_serial.hip", []), ("api", "snn_lif_api.hip", [])]
+    + [(name, f"{name}.hip", []) for name in ("seq_conv", "seq_scan_forward", "seq_scan_backward", "seq_norm",
+                                              "snn_seq_api")]
 )
 
 

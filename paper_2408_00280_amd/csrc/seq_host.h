@@ -1,0 +1,228 @@
+// Host side of the sequence operators (include/snn_seq.h): argument checks, the plans that
+// size launches and workspaces, and the entries of the kernel translation units.  Plans
+// depend only on the configuration and the shape, so that a forward, its backward and the
+// size queries agree.
+#pragma once
+#include "lif_host.h"
+#include "snn_seq.h"
+
+namespace snnlif {
+
+constexpr int64_t kMaxSeqB = int64_t(1) << 24, kMaxSeqF = int64_t(1) << 24;
+constexpr int64_t kMaxRows = int64_t(1) << 31, kMaxSpan = int64_t(1) << 44;
+constexpr int kMaxTaps = 8, kMaxStates = 64;
+
+inline snn_status check_io(int io) { return io == SNN_IO_F32 || io == SNN_IO_BF16 ? SNN_OK : SNN_E_PARAM; }
+inline int64_t elem_bytes(int io) { return io == SNN_IO_F32 ? 4 : 2; }
+
+inline snn_status check_seq_shape(int64_t T, int64_t B, int64_t F) {
+    if (T < 0 || B < 0 || F < 0 || T > kMaxT || B > kMaxSeqB || F > kMaxSeqF) return SNN_E_SHAPE;
+    if (B > 0 && T > kMaxRows / B) return SNN_E_SHAPE;
+    if (T > 0 && B > 0 && F > kMaxSpan / (T * B)) return SNN_E_SHAPE;
+    return SNN_OK;
+}
+
+// Elements that a [T][B][X] tensor spans with its steps; -1 when a step is negative or the
+// span is too long.  The step of an axis of length 1 is not used.
+inline int64_t seq_span(const snn_seq* s, int64_t T, int64_t B, int64_t X) {
+    int64_t span = X;
+    for (const auto& [n, step] : {std::pair<int64_t, int64_t>{T, s->t}, {B, s->b}}) {
+        if (n <= 1) continue;
+        if (step < 0 || step > kMaxSpan / (n - 1)) return -1;
+        span += (n - 1) * step;
+        if (span > kMaxSpan) return -1;
+    }
+    return span;
+}
+
+inline snn_status check_in(const snn_seq* s, int64_t T, int64_t B, int64_t X, int io) {
+    if (s == nullptr || s->data == nullptr) return SNN_E_NULL;
+    if (seq_span(s, T, B, X) < 0) return SNN_E_SHAPE;
+    return aligned_to(s->data, uintptr_t(elem_bytes(io))) ? SNN_OK : SNN_E_ALIGN;
+}
+
+// An output's rows must not overlap: one axis steps over rows, the other over whole runs of
+// the first.
+inline snn_status check_out(const snn_seq* s, int64_t T, int64_t B, int64_t X, int io) {
+    const snn_status st = check_in(s, T, B, X, io);
+    if (st != SNN_OK) return st;
+    const auto nested = [X](int64_t n_in, int64_t in, int64_t n_out, int64_t out) {
+        return (n_in <= 1 || in >= X) && (n_out <= 1 || out >= (n_in <= 1 ? X : (n_in - 1) * in + X));
+    };
+    return nested(B, s->b, T, s->t) || nested(T, s->t, B, s->b) ? SNN_OK : SNN_E_SHAPE;
+}
+
+inline snn_status first_error(std::initializer_list<snn_status> all) {
+    for (snn_status s : all)
+        if (s == SNN_E_NULL) return s;      // as everywhere: NULL before the rest
+    for (snn_status s : all)
+        if (s != SNN_OK) return s;
+    return SNN_OK;
+}
+
+inline snn_status need(const void* p, uintptr_t align = 4) {
+    return p == nullptr ? SNN_E_NULL : aligned_to(p, align) ? SNN_OK : SNN_E_ALIGN;
+}
+inline snn_status optional(const void* p, uintptr_t align = 4) { return p == nullptr ? SNN_OK : need(p, align); }
+
+// A [T][B][X] tensor as the kernels take it.
+struct Rows {
+    const void* p;
+    int64_t t, b;
+};
+inline Rows rows(const snn_seq* s) { return s == nullptr ? Rows{nullptr, 0, 0} : Rows{s->data, s->t, s->b}; }
+
+inline int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
+
+constexpr int64_t kMaxBlocks = INT32_MAX;
+
+// Bytes of a piece of a workspace: pieces start on 256-byte boundaries.
+inline int64_t piece(int64_t bytes) { return (bytes + 255) / 256 * 256; }
+
+// Sums of P partial results of n values each, in a fixed order: out[i] = sum_p part[p*stride + i].
+// The n values go to up to three arrays one after the other (an array may be NULL).
+struct ReduceOut {
+    float* p[3];
+    int64_t n[3];
+};
+snn_status reduce_entry(const float* part, int64_t P, int64_t stride, const ReduceOut& out, hipStream_t s);
+
+// -- convolution -------------------------------------------------------------------------
+inline snn_status check_conv_cfg(const snn_conv_cfg* c) {
+    if (c == nullptr) return SNN_E_NULL;
+    if (check_io(c->io) != SNN_OK || c->width < 1 || c->width > kMaxTaps) return SNN_E_PARAM;
+    return c->act == SNN_ACT_NONE || c->act == SNN_ACT_SILU ? SNN_OK : SNN_E_PARAM;
+}
+
+// Lanes own 16 bytes of features (the few left over one each) and walk `steps` steps of one
+// sequence; there are `chunks` such pieces of the time axis.  Eight waves per CU keep enough
+// loads in flight; shorter walks than 16 steps read too much of their neighbours' inputs.
+struct ConvPlan {
+    int64_t lanes;   // per sequence and chunk
+    int64_t steps, chunks;
+};
+
+inline int conv_vec(int io) { return io == SNN_IO_F32 ? 4 : 8; }
+
+inline ConvPlan conv_plan(const snn_conv_cfg* c, int64_t T, int64_t B, int64_t F) {
+    const int v = conv_vec(c->io);
+    ConvPlan p;
+    p.lanes = F / v + F % v;
+    const int64_t want = ceil_div(int64_t(1) << 17, p.lanes * B);
+    p.steps = std::max<int64_t>(16, ceil_div(T, want));
+    p.chunks = ceil_div(T, p.steps);
+    return p;
+}
+
+inline int64_t conv_partial(const snn_conv_cfg* c, int64_t F) { return F * (c->width + 1); }
+
+inline int64_t conv_workspace(const snn_conv_cfg* c, int64_t T, int64_t B, int64_t F) {
+    return piece(conv_plan(c, T, B, F).chunks * B * conv_partial(c, F) * 4);
+}
+
+struct ConvArgs {
+    int64_t T, B, F;
+    Rows x, y, gy, gx;      // y: forward; gy, gx: backward
+    const float* weight;
+    const float* bias;
+    const void* state_in;
+    const int32_t* lengths;
+    void* state_out;        // forward
+    const void* gstate_out; // backward
+    void* gstate_in;
+    float* part;
+    ConvPlan plan;
+};
+snn_status conv_forward_entry(const snn_conv_cfg* c, const ConvArgs& a, hipStream_t s);
+snn_status conv_backward_entry(const snn_conv_cfg* c, const ConvArgs& a, hipStream_t s);
+
+// -- scan --------------------------------------------------------------------------------
+inline snn_status check_scan_cfg(const snn_scan_cfg* c) {
+    if (c == nullptr) return SNN_E_NULL;
+    if (check_io(c->io) != SNN_OK || c->states < 1 || c->states > kMaxStates || c->groups < 1) return SNN_E_PARAM;
+    return c->softplus == 0 || c->softplus == 1 ? SNN_OK : SNN_E_PARAM;
+}
+
+// A workgroup owns 64 features of one group and one sequence, a feature per lane; each of its
+// `waves` waves holds 4 of their states.  Time goes in blocks of K steps; the forward keeps
+// the state at the start of each block but the first.
+struct ScanPlan {
+    int waves;
+    int k;
+    int sp;          // states as stored in the packed B and C: 4 per wave
+    int64_t tiles;   // workgroups per group
+    int64_t blocks;  // of K steps
+};
+
+inline ScanPlan scan_plan(const snn_scan_cfg* c, int64_t T, int64_t F) {
+    ScanPlan p;
+    p.waves = (c->states + 3) / 4;
+    p.sp = p.waves * 4;
+    p.k = c->states > 32 ? 8 : 16;
+    p.tiles = ceil_div(F / c->groups, kWave);
+    p.blocks = ceil_div(T, p.k);
+    return p;
+}
+
+inline int64_t scan_saved(const snn_scan_cfg* c, int64_t T, int64_t B, int64_t F) {
+    return (scan_plan(c, T, F).blocks - 1) * B * F * c->states * 4;
+}
+inline int64_t scan_packed(const snn_scan_cfg* c, const ScanPlan& p, int64_t T, int64_t B) {
+    return T * B * c->groups * 2 * p.sp * 4;
+}
+inline int64_t scan_forward_workspace(const snn_scan_cfg* c, int64_t T, int64_t B, int64_t F) {
+    return piece(scan_packed(c, scan_plan(c, T, F), T, B));
+}
+inline int64_t scan_partial_values(int64_t F, int S) { return F * (S + 2); }
+inline int64_t scan_backward_workspace(const snn_scan_cfg* c, int64_t T, int64_t B, int64_t F) {
+    const ScanPlan p = scan_plan(c, T, F);
+    const int64_t packed = scan_packed(c, p, T, B);
+    return piece(packed) + piece(packed * p.tiles) + piece(B * scan_partial_values(F, c->states) * 4);
+}
+
+struct ScanArgs {
+    int64_t T, B, F;
+    int S, G, softplus;
+    Rows x, dt, Bm, Cm, y, gy, gx, gdt, gB, gC;
+    const float *A, *D, *dt_bias, *h_in;
+    const int32_t* lengths;
+    float* h_out;
+    float* saved;
+    const float* gh_out;
+    float *gA, *gD, *gdt_bias, *gh_in;
+    float* packed;   // [T][B][G][2][sp]: B then C
+    float* part_bc;  // backward: the same per tile
+    float* part_f;   // backward: [B] x (A [F][S], D [F], dt_bias [F])
+    ScanPlan plan;
+};
+snn_status scan_pack_entry(int io, const ScanArgs& a, hipStream_t s);
+snn_status scan_forward_entry(int io, const ScanArgs& a, hipStream_t s);
+snn_status scan_backward_entry(int io, const ScanArgs& a, hipStream_t s);
+
+// -- norm --------------------------------------------------------------------------------
+inline snn_status check_norm_cfg(const snn_norm_cfg* c) {
+    if (c == nullptr) return SNN_E_NULL;
+    return check_io(c->io) == SNN_OK && c->eps > 0.0f && std::isfinite(c->eps) ? SNN_OK : SNN_E_PARAM;
+}
+
+// Workgroups of the backward; each walks rows g, g + groups, ... and keeps one partial sum of
+// the parameters' gradients.
+inline int64_t norm_groups(int64_t T, int64_t B) { return std::min<int64_t>(T * B, 1024); }
+inline int64_t norm_workspace(int64_t T, int64_t B, int64_t F) { return piece(norm_groups(T, B) * 3 * F * 4); }
+
+struct NormArgs {
+    int64_t T, B, F;
+    float eps;
+    Rows y, z, r, r_new, u, gr_new, gu, gy, gz, gr;
+    const float *w_post, *scale, *w_pre;
+    const int32_t* lengths;
+    const float* rstd_in;
+    float* rstd;
+    float *gw_post, *gscale, *gw_pre;
+    float* part;
+    int64_t groups;
+};
+snn_status norm_forward_entry(int io, const NormArgs& a, hipStream_t s);
+snn_status norm_backward_entry(int io, const NormArgs& a, hipStream_t s);
+
+}  // namespace snnlif

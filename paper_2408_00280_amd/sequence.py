@@ -1,0 +1,252 @@
+"""Torch-tensor conveniences over the sequence operators of include/snn_seq.h: a short causal
+convolution, a selective state space scan, and a block's gate, norm and scaled residual with
+the next block's norm.
+
+Data is [T, B, F] in float32 or bfloat16, as the LIF layers of this package take it, in any
+strides whose last axis is contiguous: time-major, batch-major (a transposed [B, T, F]) and
+slices of wider rows are read in place, anything else is copied first.  Parameters and their
+gradients are float32.  ``lengths`` (int32 [B]) gives each sequence its own number of steps:
+what lies behind is not read, and is 0 in outputs and gradients.
+
+Torch provides device memory and streams only.  Work is enqueued on torch's current stream
+of the tensors' device, or on ``stream`` (a torch.cuda.Stream or a raw handle).
+"""
+from __future__ import annotations
+
+import functools
+
+import torch
+
+from . import native
+
+IO_OF = {torch.float32: native.SNN_IO_F32, torch.bfloat16: native.SNN_IO_BF16}
+ACTS = {None: native.SNN_ACT_NONE, "silu": native.SNN_ACT_SILU}
+
+
+def _on_stream(fn):
+    """fn with its first tensor's device as the current one, on `stream`."""
+    @functools.wraps(fn)
+    def call(x, *args, stream=None, **kw):
+        if not x.is_cuda:
+            raise ValueError("tensors must be on the GPU")
+        if stream is None and x.device.index == torch._C._cuda_getDevice():
+            return fn(x, *args, **kw)
+        with torch.cuda.device(x.device):
+            if stream is None:
+                return fn(x, *args, **kw)
+            if not isinstance(stream, torch.cuda.Stream):
+                stream = torch.cuda.ExternalStream(int(stream)) if stream else torch.cuda.default_stream()
+            with torch.cuda.stream(stream):
+                return fn(x, *args, **kw)
+    return call
+
+
+def _shape(x):
+    if x.dim() != 3 or x.dtype not in IO_OF:
+        raise ValueError("data must be a float32 or bfloat16 tensor [T, B, F]")
+    return x.shape
+
+
+def _data(name, a, x, shape):
+    """`a` as [T, B, X] data that goes with x: contiguous behind the second axis."""
+    if a.dtype != x.dtype or a.device != x.device or a.shape != shape:
+        raise ValueError(f"{name} must be a {x.dtype} tensor of shape {tuple(shape)} on {x.device}")
+    n = 1
+    for size, step in zip(reversed(shape[2:]), reversed(a.stride()[2:])):
+        if size != 1 and step != n:
+            return a.contiguous()
+        n *= size
+    return a
+
+
+def _dense(name, a, x, shape, dtype=torch.float32):
+    if a is None:
+        return None
+    if a.dtype != dtype or a.device != x.device or a.shape != shape or not a.is_contiguous():
+        raise ValueError(f"{name} must be a contiguous {dtype} tensor of shape {tuple(shape)} on {x.device}")
+    return a
+
+
+def _like(x, shape=None):
+    """Uninitialised data of the given shape, time-major or batch-major as x is."""
+    shape = x.shape if shape is None else shape
+    if x.stride(0) < x.stride(1) and shape[0] > 1 and shape[1] > 1:
+        return torch.empty((shape[1], shape[0], *shape[2:]), dtype=x.dtype, device=x.device).transpose(0, 1)
+    return torch.empty(shape, dtype=x.dtype, device=x.device)
+
+
+def _bytes(n, x):
+    return torch.empty(n, dtype=torch.uint8, device=x.device) if n else None
+
+
+def _params(shape, x, empty):
+    """A parameter's gradient: the kernels write it whole, unless there is nothing to do."""
+    return (torch.zeros if empty else torch.empty)(shape, dtype=torch.float32, device=x.device)
+
+
+def _hand_over(out, given):
+    """No steps: the state out is the state in."""
+    if out is not None and out is not given:
+        out.zero_() if given is None else out.copy_(given)
+
+
+# ---------------------------------------------------------------------------------------
+
+def _conv_args(x, weight, bias, act, state, lengths):
+    T, B, F = _shape(x)
+    if weight.dim() != 2 or act not in ACTS:
+        raise ValueError("weight must be [F, W], act None or 'silu'")
+    W = weight.shape[1]
+    x = _data("x", x, x, (T, B, F))
+    _dense("weight", weight, x, (F, W))
+    _dense("bias", bias, x, (F,))
+    _dense("state", state, x, (W - 1, B, F), x.dtype)
+    _dense("lengths", lengths, x, (B,), torch.int32)
+    return x, T, B, F, W, native.snn_conv_cfg(IO_OF[x.dtype], W, ACTS[act])
+
+
+@_on_stream
+def conv_forward(x, weight, bias=None, *, act="silu", state=None, state_out=None, lengths=None):
+    """Causal convolution of x[T, B, F] along time with weight[F, W] (W up to 8, the last tap
+    on the current step), bias[F] and activation: y.  state ([W-1, B, F]): the inputs before
+    step 0; state_out: written with the last W-1 inputs, may be `state` (in place)."""
+    x, T, B, F, W, cfg = _conv_args(x, weight, bias, act, state, lengths)
+    _dense("state_out", state_out, x, (W - 1, B, F), x.dtype)
+    y = _like(x)
+    if x.numel():
+        native.snn_conv_forward(cfg, T, B, F, x, weight, bias, state, lengths, y, state_out)
+    else:
+        _hand_over(state_out, state)
+    return y
+
+
+@_on_stream
+def conv_backward(x, weight, bias, grad_y, *, act="silu", state=None, lengths=None, grad_state_out=None):
+    """Gradients (x, weight, bias or None, state or None) of conv_forward with the same
+    arguments; grad_state_out: the gradient of its state_out."""
+    x, T, B, F, W, cfg = _conv_args(x, weight, bias, act, state, lengths)
+    gy = _data("grad_y", grad_y, x, (T, B, F))
+    _dense("grad_state_out", grad_state_out, x, (W - 1, B, F), x.dtype)
+    empty = not x.numel()
+    gx, gw = _like(x), _params((F, W), x, empty)
+    gb = None if bias is None else _params((F,), x, empty)
+    gs = None if state is None else torch.empty_like(state)
+    if empty:
+        _hand_over(gs, grad_state_out)
+    else:
+        ws = _bytes(native.snn_conv_workspace_bytes(cfg, T, B, F), x)
+        native.snn_conv_backward(cfg, T, B, F, x, weight, bias, state, lengths, gy, grad_state_out, gx, gw, gb, gs, ws)
+    return gx, gw, gb, gs
+
+
+# ---------------------------------------------------------------------------------------
+
+def _scan_args(x, dt, A, Bm, Cm, D, dt_bias, softplus, h_in, lengths):
+    T, B, F = _shape(x)
+    if Bm.dim() != 4 or A.dim() != 2:
+        raise ValueError("A must be [F, S], Bm and Cm [T, B, G, S]")
+    G, S = Bm.shape[2:]
+    x, dt = _data("x", x, x, (T, B, F)), _data("dt", dt, x, (T, B, F))
+    Bm, Cm = _data("Bm", Bm, x, (T, B, G, S)), _data("Cm", Cm, x, (T, B, G, S))
+    _dense("A", A, x, (F, S))
+    _dense("D", D, x, (F,))
+    _dense("dt_bias", dt_bias, x, (F,))
+    _dense("h_in", h_in, x, (B, F, S))
+    _dense("lengths", lengths, x, (B,), torch.int32)
+    cfg = native.snn_scan_cfg(IO_OF[x.dtype], S, G, int(bool(softplus)))
+    return (x, dt, A, Bm, Cm, D, dt_bias, h_in, lengths), (T, B, F, G, S), cfg
+
+
+@_on_stream
+def scan_forward(x, dt, A, Bm, Cm, D=None, dt_bias=None, *, softplus=True, h_in=None, h_out=None, lengths=None,
+                 train=False):
+    """Selective scan of x[T, B, F] with steps softplus(dt + dt_bias) (dt [T, B, F], dt_bias
+    [F]), rates A [F, S], Bm and Cm [T, B, G, S] (shared by the F/G features of a group) and
+    skip weights D [F].  h_in, h_out ([B, F, S] float32): the state before step 0 and after
+    the last, h_out is written and may be h_in (in place).  Returns (y, saved), saved for
+    scan_backward with train=True and None otherwise."""
+    args, (T, B, F, G, S), cfg = _scan_args(x, dt, A, Bm, Cm, D, dt_bias, softplus, h_in, lengths)
+    x = args[0]
+    _dense("h_out", h_out, x, (B, F, S))
+    if train and h_out is not None and h_out is h_in:
+        raise ValueError("the backward reads h_in: h_out must be another tensor")
+    y = _like(x)
+    saved = torch.empty(native.snn_scan_saved_bytes(cfg, T, B, F), dtype=torch.uint8, device=x.device) if train else None
+    if x.numel():
+        ws = _bytes(native.snn_scan_workspace_bytes(cfg, T, B, F)[0], x)
+        native.snn_scan_forward(cfg, T, B, F, *args, y, h_out, saved if train and saved.numel() else None, ws)
+    else:
+        _hand_over(h_out, h_in)
+    return y, saved
+
+
+@_on_stream
+def scan_backward(x, dt, A, Bm, Cm, D, dt_bias, saved, grad_y, *, softplus=True, h_in=None, lengths=None,
+                  grad_h_out=None):
+    """Gradients (x, dt, A, Bm, Cm, D or None, dt_bias or None, h_in or None) of scan_forward
+    with the same arguments and what it saved; grad_h_out: the gradient of its h_out."""
+    args, (T, B, F, G, S), cfg = _scan_args(x, dt, A, Bm, Cm, D, dt_bias, softplus, h_in, lengths)
+    x = args[0]
+    if saved.dtype != torch.uint8 or saved.numel() != native.snn_scan_saved_bytes(cfg, T, B, F):
+        raise ValueError("saved must be what scan_forward(train=True) returned for these arguments")
+    gy = _data("grad_y", grad_y, x, (T, B, F))
+    _dense("grad_h_out", grad_h_out, x, (B, F, S))
+    empty = not x.numel()
+    gx, gdt, gB, gC = _like(x), _like(x), _like(x, (T, B, G, S)), _like(x, (T, B, G, S))
+    gA = _params((F, S), x, empty)
+    gD = None if D is None else _params((F,), x, empty)
+    gbias = None if dt_bias is None else _params((F,), x, empty)
+    gh = None if h_in is None else torch.empty_like(h_in)
+    if empty:
+        gB.zero_(), gC.zero_()
+        _hand_over(gh, grad_h_out)
+    else:
+        ws = _bytes(native.snn_scan_workspace_bytes(cfg, T, B, F)[1], x)
+        native.snn_scan_backward(cfg, T, B, F, *args, saved if saved.numel() else None, gy, grad_h_out, gx, gdt, gA, gB,
+                                 gC, gD, gbias, gh, ws)
+    return gx, gdt, gA, gB, gC, gD, gbias, gh
+
+
+# ---------------------------------------------------------------------------------------
+
+def _norm_args(y, r, z, w_post, scale, w_pre, eps, lengths):
+    T, B, F = _shape(y)
+    y = _data("y", y, y, (T, B, F))
+    r = None if r is None else _data("r", r, y, (T, B, F))
+    z = None if z is None else _data("z", z, y, (T, B, F))
+    for name, w in (("w_post", w_post), ("scale", scale), ("w_pre", w_pre)):
+        _dense(name, w, y, (F,))
+    _dense("lengths", lengths, y, (B,), torch.int32)
+    return (y, z, r, w_post, scale, w_pre, lengths), (T, B, F), native.snn_norm_cfg(IO_OF[y.dtype], eps)
+
+
+@_on_stream
+def norm_forward(y, r=None, z=None, w_post=None, scale=None, w_pre=None, *, eps=1e-5, lengths=None, train=False):
+    """The end of a block and the start of the next over the last axis of y[T, B, F]:
+    r_new = r + scale * norm(y * silu(z)) and u = norm(r_new), root-mean-square norms with the
+    weights w_post and w_pre.  Without z, w_post, scale, r or w_pre that part is left out.
+    Returns (r_new, u or None, rstd), rstd for norm_backward with train=True, else None."""
+    args, (T, B, F), cfg = _norm_args(y, r, z, w_post, scale, w_pre, eps, lengths)
+    r_new, u = _like(args[0]), None if w_pre is None else _like(args[0])
+    rstd = torch.empty((2, T, B), dtype=torch.float32, device=y.device) if train else None
+    if y.numel():
+        native.snn_norm_forward(cfg, T, B, F, *args, r_new, u, rstd)
+    return r_new, u, rstd
+
+
+@_on_stream
+def norm_backward(y, r, z, w_post, scale, w_pre, rstd, grad_r_new, grad_u=None, *, eps=1e-5, lengths=None):
+    """Gradients (y, r, z, w_post, scale, w_pre; None where the input is None) of norm_forward
+    with the same arguments and its rstd.  grad_r_new or grad_u may be None (no gradient)."""
+    args, (T, B, F), cfg = _norm_args(y, r, z, w_post, scale, w_pre, eps, lengths)
+    y = args[0]
+    _dense("rstd", rstd, y, (2, T, B))
+    g1 = None if grad_r_new is None else _data("grad_r_new", grad_r_new, y, (T, B, F))
+    g2 = None if grad_u is None else _data("grad_u", grad_u, y, (T, B, F))
+    empty = not y.numel()
+    gy, gr, gz = (None if a is None else _like(a) for a in (args[0], args[2], args[1]))
+    gw = [None if w is None else _params((F,), y, empty) for w in (w_post, scale, w_pre)]
+    if not empty:
+        ws = _bytes(native.snn_norm_workspace_bytes(cfg, T, B, F), y)
+        native.snn_norm_backward(cfg, T, B, F, *args, rstd, g1, g2, gy, gz, gr, *gw, ws)
+    return gy, gr, gz, *gw
