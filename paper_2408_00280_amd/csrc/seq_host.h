@@ -8,7 +8,7 @@
 
 namespace snnlif {
 
-constexpr int64_t kMaxSeqB = int64_t(1) << 24, kMaxSeqF = int64_t(1) << 24;
+constexpr int64_t kMaxSeqT = int64_t(1) << 30, kMaxSeqB = int64_t(1) << 24, kMaxSeqF = int64_t(1) << 24;
 constexpr int64_t kMaxRows = int64_t(1) << 31, kMaxSpan = int64_t(1) << 44;
 constexpr int kMaxTaps = 8, kMaxStates = 64;
 
@@ -16,7 +16,7 @@ inline snn_status check_io(int io) { return io == SNN_IO_F32 || io == SNN_IO_BF1
 inline int64_t elem_bytes(int io) { return io == SNN_IO_F32 ? 4 : 2; }
 
 inline snn_status check_seq_shape(int64_t T, int64_t B, int64_t F) {
-    if (T < 0 || B < 0 || F < 0 || T > kMaxT || B > kMaxSeqB || F > kMaxSeqF) return SNN_E_SHAPE;
+    if (T < 0 || B < 0 || F < 0 || T > kMaxSeqT || B > kMaxSeqB || F > kMaxSeqF) return SNN_E_SHAPE;
     if (B > 0 && T > kMaxRows / B) return SNN_E_SHAPE;
     if (T > 0 && B > 0 && F > kMaxSpan / (T * B)) return SNN_E_SHAPE;
     return SNN_OK;
@@ -143,41 +143,46 @@ inline snn_status check_scan_cfg(const snn_scan_cfg* c) {
     return c->softplus == 0 || c->softplus == 1 ? SNN_OK : SNN_E_PARAM;
 }
 
+constexpr int kScanStates = 4;   // states per lane
+constexpr int kScanBlock = 8;    // steps that the waves share out at a time
+
 // A workgroup owns 64 features of one group and one sequence, a feature per lane; each of its
-// `waves` waves holds 4 of their states.  Time goes in blocks of K steps; the forward keeps
-// the state at the start of each block but the first.
+// `waves` (a power of two) waves holds 4 of their states.  The forward keeps the state every
+// `keep` steps for the backward, which holds that many steps' decays in registers: 16, but 8
+// where 16 waves leave a wave half the registers, and where 1 or 2 waves stage a block's steps.
 struct ScanPlan {
     int waves;
-    int k;
-    int sp;          // states as stored in the packed B and C: 4 per wave
-    int64_t tiles;   // workgroups per group
-    int64_t blocks;  // of K steps
+    int keep;
+    int64_t tiles;      // workgroups per group
+    int64_t steps;      // per segment of the time axis
+    int64_t segments;
 };
 
-inline ScanPlan scan_plan(const snn_scan_cfg* c, int64_t T, int64_t F) {
+constexpr int scan_keep(int waves) { return waves == 4 || waves == 8 ? 16 : 8; }
+
+inline ScanPlan scan_plan(const snn_scan_cfg* c, int64_t T, int64_t B, int64_t F) {
     ScanPlan p;
-    p.waves = (c->states + 3) / 4;
-    p.sp = p.waves * 4;
-    p.k = c->states > 32 ? 8 : 16;
+    p.waves = 1;
+    while (p.waves * kScanStates < c->states) p.waves *= 2;
+    p.keep = scan_keep(p.waves);
     p.tiles = ceil_div(F / c->groups, kWave);
-    p.blocks = ceil_div(T, p.k);
+    p.segments = 1;
+    p.steps = T;
     return p;
 }
 
 inline int64_t scan_saved(const snn_scan_cfg* c, int64_t T, int64_t B, int64_t F) {
-    return (scan_plan(c, T, F).blocks - 1) * B * F * c->states * 4;
+    const int64_t states = ceil_div(c->states, kScanStates) * kScanStates;
+    return (ceil_div(T, scan_plan(c, T, B, F).keep) - 1) * B * F * states * 4;
 }
-inline int64_t scan_packed(const snn_scan_cfg* c, const ScanPlan& p, int64_t T, int64_t B) {
-    return T * B * c->groups * 2 * p.sp * 4;
+inline int64_t scan_forward_workspace(const snn_scan_cfg* c, int64_t T, int64_t B, int64_t F) { return 0; }
+constexpr int64_t scan_partial_values(int64_t F, int S) { return F * (S + 2); }
+// dL/dB and dL/dC of every tile, as the waves hold them.
+inline int64_t scan_partial_bc(const snn_scan_cfg* c, const ScanPlan& p, int64_t T, int64_t B) {
+    return p.tiles * T * B * c->groups * p.waves * 2 * kScanStates * 4;
 }
-inline int64_t scan_forward_workspace(const snn_scan_cfg* c, int64_t T, int64_t B, int64_t F) {
-    return piece(scan_packed(c, scan_plan(c, T, F), T, B));
-}
-inline int64_t scan_partial_values(int64_t F, int S) { return F * (S + 2); }
 inline int64_t scan_backward_workspace(const snn_scan_cfg* c, int64_t T, int64_t B, int64_t F) {
-    const ScanPlan p = scan_plan(c, T, F);
-    const int64_t packed = scan_packed(c, p, T, B);
-    return piece(packed) + piece(packed * p.tiles) + piece(B * scan_partial_values(F, c->states) * 4);
+    return piece(scan_partial_bc(c, scan_plan(c, T, B, F), T, B)) + piece(B * scan_partial_values(F, c->states) * 4);
 }
 
 struct ScanArgs {
@@ -190,12 +195,10 @@ struct ScanArgs {
     float* saved;
     const float* gh_out;
     float *gA, *gD, *gdt_bias, *gh_in;
-    float* packed;   // [T][B][G][2][sp]: B then C
-    float* part_bc;  // backward: the same per tile
+    float* part_bc;  // backward: [tiles][T][B][G][waves][B, C][4]
     float* part_f;   // backward: [B] x (A [F][S], D [F], dt_bias [F])
     ScanPlan plan;
 };
-snn_status scan_pack_entry(int io, const ScanArgs& a, hipStream_t s);
 snn_status scan_forward_entry(int io, const ScanArgs& a, hipStream_t s);
 snn_status scan_backward_entry(int io, const ScanArgs& a, hipStream_t s);
 

@@ -4,67 +4,132 @@
 
 namespace snnlif {
 
-constexpr int kSL = 4;   // states per lane
+constexpr int kSL = kScanStates;   // states per lane
 
-// B and C of one step and group are the same for every lane of a wave: they are packed
-// beforehand as float32 (4 per wave, zeros behind the last state) and read through the scalar
-// cache, so that they cost no vector register and no vector instruction.
-typedef const __attribute__((address_space(4))) f32x4_t* scalar_f32x4;
-
-__device__ __forceinline__ f32x4_t scalar_load4(const float* p) {
-    return *(scalar_f32x4)(reinterpret_cast<uintptr_t>(p));
-}
-
-// The workgroup's place: 64 features of a group, one sequence.
+// The workgroup's place: 64 features of a group, one sequence, one segment of its steps.
 struct ScanPlace {
     int lane, wave;
     int64_t g, tile, b;
     int64_t f;        // this lane's feature (the group's last for lanes behind it)
     bool active;
+    int first, states;   // this wave's states
+    int t0, t1, len;     // the segment, and the steps of the sequence
 };
 
 __device__ __forceinline__ ScanPlace scan_place(const ScanArgs& a) {
     ScanPlace p;
     p.lane = threadIdx.x & (kWave - 1);
     p.wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
-    const int64_t i = blockIdx.x, per = a.F / a.G;
-    p.tile = i % a.plan.tiles;
-    p.g = i / a.plan.tiles % a.G;
-    p.b = i / (a.plan.tiles * a.G);
-    const int64_t j = p.tile * kWave + p.lane;
+    const unsigned i = blockIdx.x, tiles = unsigned(a.plan.tiles), per = unsigned(a.F / a.G);
+    const unsigned q = i / tiles;
+    p.tile = i % tiles;
+    p.g = q % unsigned(a.G);
+    p.b = q / unsigned(a.G);
+    const unsigned j = unsigned(p.tile) * kWave + p.lane;
     p.active = j < per;
     p.f = p.g * per + (p.active ? j : per - 1);
+    p.first = p.wave * kSL;
+    p.states = min(kSL, a.S - p.first);
+    p.t0 = int(blockIdx.y * a.plan.steps);
+    p.t1 = int(min(a.T, p.t0 + a.plan.steps));
+    p.len = __builtin_amdgcn_readfirstlane(steps_of(a.lengths, p.b, a.T));
     return p;
 }
 
 // A[f][n] log2(e) of the lane's states, 0 behind the last (whose state then stays 0).
 __device__ __forceinline__ void load_rates(const ScanArgs& a, const ScanPlace& p, float (&r)[kSL]) {
 #pragma unroll
-    for (int i = 0; i < kSL; ++i) {
-        const int n = p.wave * kSL + i;
-        r[i] = n < a.S ? a.A[p.f * a.S + n] * kLog2e : 0.0f;
-    }
+    for (int i = 0; i < kSL; ++i) r[i] = i < p.states ? a.A[p.f * a.S + p.first + i] * kLog2e : 0.0f;
 }
 
 __device__ __forceinline__ void load_state(const ScanArgs& a, const ScanPlace& p, const float* from, float (&h)[kSL]) {
 #pragma unroll
-    for (int i = 0; i < kSL; ++i) {
-        const int n = p.wave * kSL + i;
-        h[i] = from != nullptr && n < a.S ? from[(p.b * a.F + p.f) * a.S + n] : 0.0f;
-    }
+    for (int i = 0; i < kSL; ++i)
+        h[i] = from != nullptr && i < p.states ? from[(p.b * a.F + p.f) * a.S + p.first + i] : 0.0f;
 }
 
 __device__ __forceinline__ void store_state(const ScanArgs& a, const ScanPlace& p, float* to, const float (&h)[kSL]) {
 #pragma unroll
-    for (int i = 0; i < kSL; ++i) {
-        const int n = p.wave * kSL + i;
-        if (p.active && n < a.S) to[(p.b * a.F + p.f) * a.S + n] = h[i];
-    }
+    for (int i = 0; i < kSL; ++i)
+        if (p.active && i < p.states) to[(p.b * a.F + p.f) * a.S + p.first + i] = h[i];
 }
 
-// The state kept at the start of block c >= 1: [c-1][b][n][f].
-__device__ __forceinline__ int64_t kept_at(const ScanArgs& a, const ScanPlace& p, int64_t c, int n) {
-    return (((c - 1) * a.B + p.b) * a.S + n) * a.F + p.f;
+// States by piece c of the time axis, features next to each other and whole waves' states:
+// [c][b][wave][4][f].
+struct StateColumn {
+    float* p;
+    int64_t piece, F;
+    __device__ StateColumn(const ScanArgs& a, const ScanPlace& s, float* base) : F(a.F) {
+        const int64_t waves = (a.S + kSL - 1) / kSL;
+        p = base + (s.b * waves + s.wave) * kSL * F + s.f;
+        piece = a.B * waves * kSL * F;
+    }
+    __device__ void load(int64_t c, float (&h)[kSL]) const {
+#pragma unroll
+        for (int i = 0; i < kSL; ++i) h[i] = p[c * piece + i * F];
+    }
+    __device__ void store(int64_t c, const float (&h)[kSL]) const {
+#pragma unroll
+        for (int i = 0; i < kSL; ++i) p[c * piece + i * F] = h[i];
+    }
+};
+
+// A lane's column of a [T][B][F] tensor.
+template <int IO>
+struct Column {
+    static constexpr int kBytes = IO == SNN_IO_F32 ? 4 : 2;
+    const char* p;
+    int64_t step;    // bytes
+    __device__ Column(const Rows& r, const ScanPlace& s) : p(static_cast<const char*>(at<IO>(r, 0, s.b, s.f))), step(r.t * kBytes) {}
+    __device__ auto load(int t) const { return IoVec<IO, 1>::load(p + t * step, 0); }
+    __device__ void store(int t, float v) const { store1<IO>(const_cast<char*>(p) + t * step, v); }
+};
+
+// B and C of one step and group are the same for every lane of a wave.  Each block of steps is
+// staged in LDS as float32, 4 of B and 4 of C per wave (zeros behind the last state and behind
+// the sequence's end), one value per thread (two in 16-step blocks), and read back 16 bytes at a
+// time with every lane at the same address.  Scalar loads, which would need no vector register,
+// take too long to come to hide behind the few steps whose values fit the scalar registers.
+template <int NS, int K>
+struct StagedBC {
+    static constexpr int N = K * 2 * kSL / kWave;    // values per thread
+    float v[K][NS][2 * kSL];
+};
+
+template <int IO, int NS, int K>
+struct BCColumns {
+    static constexpr int N = StagedBC<NS, K>::N, kApart = kWave / (2 * kSL);   // steps between a thread's values
+    const char* p;
+    int64_t step;
+    int k;
+    bool in;
+    typename IoVec<IO, 1>::raw raw[N];
+    __device__ BCColumns(const ScanArgs& a, const ScanPlace& s) {
+        const int j = threadIdx.x % (NS * 2 * kSL), n = j / (2 * kSL) * kSL + j % kSL;
+        const Rows& r = (j & kSL) ? a.Cm : a.Bm;
+        k = threadIdx.x / (NS * 2 * kSL);
+        in = n < a.S;
+        step = r.t * (IO == SNN_IO_F32 ? 4 : 2);
+        p = static_cast<const char*>(at<IO>(r, k, s.b, s.g * a.S + (in ? n : 0)));
+    }
+    __device__ void fetch(int t0, int len) {
+#pragma unroll
+        for (int i = 0; i < N; ++i)
+            if (in && t0 + k + i * kApart < len) raw[i] = IoVec<IO, 1>::load(p + (t0 + i * kApart) * step, 0);
+    }
+    __device__ void stage(int t0, int len, StagedBC<NS, K>& to) const {
+#pragma unroll
+        for (int i = 0; i < N; ++i)
+            to.v[i * kApart + k][0][threadIdx.x % (NS * 2 * kSL)] =
+                in && t0 + k + i * kApart < len ? IoVec<IO, 1>::get(raw[i], 0) : 0.0f;
+    }
+};
+
+// A barrier that orders the LDS only: loads from memory stay in flight over it.
+__device__ __forceinline__ void lds_barrier() {
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup", "local");
+    __builtin_amdgcn_s_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
 }
 
 }  // namespace snnlif

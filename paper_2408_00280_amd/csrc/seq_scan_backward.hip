@@ -6,11 +6,12 @@
 //   dL/dx = sum_n dL/dh B d + D dL/dy,  dL/ddt = dL/d(d) sigmoid(dt + dt_bias).
 // Blocks of K steps go in reverse: from the state that the forward kept at the block's start
 // the decays a and the products a h[t-1] of its steps are formed again in registers, then the
-// recurrence runs down.  Lanes, waves and scalars are as in the forward.  The sums of dL/dB
-// and dL/dC over the 64 features of a wave halve the number of values at each of the first
-// three steps (8 values and 64 lanes to 1 value in 8 groups of lanes): 17 instructions for 4
-// states.  Sums over tiles, sequences and steps go through partial results that further
-// kernels add up in a fixed order.  Bound by the vector ALU.
+// recurrence runs down.  Lanes, waves and scalars are as in the forward, and as there the next
+// block is staged and the one after is loaded while a block runs.  The sums of dL/dB and dL/dC
+// over the 64 features of a wave halve the number of values at each of the first three steps
+// (8 values and 64 lanes to 1 value in 8 groups of lanes): 17 instructions for 4 states.  Sums
+// over tiles, sequences and steps go through partial results that further kernels add up in a
+// fixed order.  Bound by the vector ALU.
 #include "seq_scan.h"
 
 namespace snnlif {
@@ -37,132 +38,218 @@ __device__ __forceinline__ float reduce8(const float (&v)[8], int lane) {
     return r;
 }
 
-template <int IO, int K>
-__global__ __launch_bounds__(K == 16 ? 512 : 1024) void scan_backward_kernel(ScanArgs a) {
-    extern __shared__ float lds[];
+struct Step {
+    float d, dx, gy;    // d, d x, dL/dy
+};
+
+template <int NS>
+struct BackwardLds {
+    static constexpr int K = scan_keep(NS);
+    Step sd[2][K][kWave];        // this block's, and the next one's as it is staged
+    StagedBC<NS, K> sbc[2];
+    float2 sg[NS][K][kWave];     // (sum dh B, sum dh a h A log2 e)
+    float sgbc[K][NS][2 * kSL];  // dL/dB and dL/dC
+};
+
+template <int IO, int NS>
+__global__ __launch_bounds__(NS * kWave, NS > 8 ? 4 : 2) void scan_backward_kernel(ScanArgs a) {
+    constexpr int K = scan_keep(NS), R = K > NS ? K / NS : 1, U = 1;
+    extern __shared__ __align__(16) char lds[];
+    auto& m = *reinterpret_cast<BackwardLds<NS>*>(lds);
     const ScanPlace p = scan_place(a);
-    const int waves = a.plan.waves, sp = a.plan.sp;
-    f32x4_t* sd = reinterpret_cast<f32x4_t*>(lds);               // [K][64] (d, d x, dL/dy, x)
-    float2* sg = reinterpret_cast<float2*>(lds + K * kWave * 4); // [waves][K][64] (sum dh B, sum dh a h A)
-    float* sbc = lds + K * kWave * (4 + 2 * waves);              // [K][2][sp]
     float rate[kSL], e[kSL], gA[kSL], gD = 0.0f, gbias = 0.0f;
     load_rates(a, p, rate);
     load_state(a, p, a.gh_out, e);
 #pragma unroll
     for (int i = 0; i < kSL; ++i) gA[i] = 0.0f;
     const float skip = a.D != nullptr ? a.D[p.f] : 0.0f, bias = a.dt_bias != nullptr ? a.dt_bias[p.f] : 0.0f;
-    const int64_t len = steps_of(a.lengths, p.b, a.T);
-    const int64_t row = int64_t(a.G) * 2 * sp;
-    // partial sums of this tile: [tile][t][b][g][2][sp]
-    float* part = a.part_bc + p.tile * a.T * a.B * row;
+    const Column<IO> cx(a.x, p), cdt(a.dt, p), cgy(a.gy, p), cgx(a.gx, p), cgdt(a.gdt, p);
+    BCColumns<IO, NS, K> cbc(a, p);
+    const bool busy = p.states > 0;
+    const int used = (a.S + kSL - 1) / kSL;
 
-    for (int64_t c = a.plan.blocks - 1; c >= 0; --c) {
-        const int64_t t0 = c * K;
-        const int n = int(max(int64_t(0), min(int64_t(K), len - t0)));
-        for (int k = p.wave; k < K; k += waves) {
-            f32x4_t d = {0.0f, 0.0f, 0.0f, 0.0f};
-            if (k < n) {
-                const float v = load1<IO>(at<IO>(a.dt, t0 + k, p.b, p.f)) + bias;
-                d[3] = load1<IO>(at<IO>(a.x, t0 + k, p.b, p.f));
-                d[2] = p.active ? load1<IO>(at<IO>(a.gy, t0 + k, p.b, p.f)) : 0.0f;
-                d[0] = a.softplus ? softplus(v) : v;
-                d[1] = p.active ? d[0] * d[3] : 0.0f;            // lanes behind the group add nothing
-            }
-            sd[k * kWave + p.lane] = d;
+    struct Raw {
+        typename IoVec<IO, 1>::raw x, dt, gy;
+    };
+    Raw raw[R], own[R];          // of the next block; of this block, for its end
+    const auto fetch = [&](int t0) {
+        if (t0 >= p.t0) cbc.fetch(t0, p.len);
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+            const int k = p.wave + r * NS;
+            if (k < K && t0 >= p.t0 && t0 + k < p.len) raw[r] = {cx.load(t0 + k), cdt.load(t0 + k), cgy.load(t0 + k)};
         }
-        __syncthreads();
-        if (n > 0) {
-            float dec[K][kSL], ah[K][kSL], h[kSL];
-            const float* bc = a.packed + (t0 * a.B + p.b) * row + p.g * 2 * sp + p.wave * kSL;
-            if (c > 0) {
+    };
+    const auto stage = [&](int t0, int to) {
+        if (t0 >= p.t0) cbc.stage(t0, p.len, m.sbc[to]);
 #pragma unroll
-                for (int i = 0; i < kSL; ++i) {
-                    const int s = p.wave * kSL + i;
-                    h[i] = s < a.S ? a.saved[kept_at(a, p, c, s)] : 0.0f;
+        for (int r = 0; r < R; ++r) {
+            const int k = p.wave + r * NS;
+            Step d = {0.0f, 0.0f, 0.0f};
+            if (k < K && t0 >= p.t0 && t0 + k < p.len) {
+                const float v = IoVec<IO, 1>::get(raw[r].dt, 0) + bias, x = IoVec<IO, 1>::get(raw[r].x, 0);
+                d.d = a.softplus ? softplus(v) : v;
+                if (p.active) {                  // lanes behind the group add nothing
+                    d.dx = d.d * x;
+                    d.gy = IoVec<IO, 1>::get(raw[r].gy, 0);
                 }
-            } else {
-                load_state(a, p, a.h_in, h);
             }
+            if (k < K) m.sd[to][k][p.lane] = d;
+        }
+    };
+    const StateColumn kept(a, p, a.saved);
+
+    int t0 = p.t0 + (p.t1 - 1 - p.t0) / K * K;
+    for (; t0 >= p.t0 && t0 >= p.len; t0 -= K) {     // blocks behind the sequence's end
+        for (int k = p.wave; k < K && t0 + k < p.t1; k += NS) {
+            if (p.active) {
+                cgx.store(t0 + k, 0.0f);
+                cgdt.store(t0 + k, 0.0f);
+            }
+        }
+    }
+    fetch(t0);
+    stage(t0, 0);
 #pragma unroll
-            for (int k = 0; k < K; ++k) {
-                if (k < n) {
-                    const f32x4_t d = sd[k * kWave + p.lane];
-                    const f32x4_t bv = scalar_load4(bc + k * a.B * row);
+    for (int r = 0; r < R; ++r) own[r] = raw[r];
+    fetch(t0 - K);
+    float h[kSL], h_next[kSL];
+    struct Ahead {
+        Step d;
+        f32x4_t b, c;
+    } step[U], ahead[U];
+    const auto read = [&](int block, int k) {
+        const f32x4_t* bc = reinterpret_cast<const f32x4_t*>(m.sbc[block].v[k][p.wave]);
+        return Ahead{m.sd[block][k][p.lane], bc[0], bc[1]};
+    };
+    if (t0 > 0 && busy) kept.load(t0 / K - 1, h);
+    else load_state(a, p, a.h_in, h);
+    lds_barrier();
+    int buf = 0;
+    for (; t0 >= p.t0; t0 -= K) {
+        const int below = max(t0 - K, p.t0);
+        Raw staged[R];
+        stage(t0 - K, buf ^ 1);
 #pragma unroll
-                    for (int i = 0; i < kSL; ++i) {
-                        dec[k][i] = __builtin_amdgcn_exp2f(d[0] * rate[i]);
-                        ah[k][i] = dec[k][i] * h[i];
-                        h[i] = fmaf(d[1], bv[i], ah[k][i]);
+        for (int r = 0; r < R; ++r) staged[r] = raw[r];
+        fetch(t0 - 2 * K);
+        if (busy) {
+#pragma unroll
+            for (int i = 0; i < U; ++i) step[i] = read(buf, i);
+            if (below > 0) kept.load(below / K - 1, h_next);
+            else load_state(a, p, a.h_in, h_next);
+            float dec[K][kSL], ah[K][kSL];
+#pragma unroll
+            for (int u = 0; u < K; u += U) {
+                if (u + U < K) {
+#pragma unroll
+                    for (int i = 0; i < U; ++i) ahead[i] = read(buf, u + U + i);
+                }
+                __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+                for (int i = 0; i < U; ++i) {
+#pragma unroll
+                    for (int s = 0; s < kSL; ++s) {
+                        dec[u + i][s] = __builtin_amdgcn_exp2f(step[i].d.d * rate[s]);
+                        ah[u + i][s] = dec[u + i][s] * h[s];
+                        h[s] = fmaf(step[i].d.dx, step[i].b[s], ah[u + i][s]);
                     }
                 }
+                __builtin_amdgcn_sched_barrier(0);
+                if (u + U < K) {
+#pragma unroll
+                    for (int i = 0; i < U; ++i) step[i] = ahead[i];
+                }
             }
 #pragma unroll
-            for (int k = K - 1; k >= 0; --k) {
-                if (k < n) {
-                    const f32x4_t d = sd[k * kWave + p.lane];
-                    const f32x4_t bv = scalar_load4(bc + k * a.B * row), cv = scalar_load4(bc + k * a.B * row + sp);
+            for (int u = K - U; u >= 0; u -= U) {
+                if (u > 0) {
+#pragma unroll
+                    for (int i = 0; i < U; ++i) ahead[i] = read(buf, u - U + i);
+                }
+                __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+                for (int i = U - 1; i >= 0; --i) {
+                    const Step d = step[i].d;
                     float v[8], gx = 0.0f, gd = 0.0f;
 #pragma unroll
-                    for (int i = 0; i < kSL; ++i) {
-                        const float dh = fmaf(cv[i], d[2], e[i]);
-                        v[i] = dh * d[1];
-                        v[kSL + i] = d[2] * fmaf(d[1], bv[i], ah[k][i]);
-                        gx = fmaf(dh, bv[i], gx);
-                        const float q = dh * ah[k][i];
-                        gd = fmaf(q, rate[i], gd);
-                        gA[i] = fmaf(q, d[0], gA[i]);
-                        e[i] = dec[k][i] * dh;
+                    for (int s = 0; s < kSL; ++s) {
+                        const float b = step[i].b[s], dh = fmaf(step[i].c[s], d.gy, e[s]);
+                        v[s] = dh * d.dx;
+                        v[kSL + s] = d.gy * fmaf(d.dx, b, ah[u + i][s]);
+                        gx = fmaf(dh, b, gx);
+                        const float q = dh * ah[u + i][s];
+                        gd = fmaf(q, rate[s], gd);
+                        gA[s] = fmaf(q, d.d, gA[s]);
+                        e[s] = dec[u + i][s] * dh;
                     }
-                    sg[(p.wave * K + k) * kWave + p.lane] = {gx, gd};
+                    m.sg[p.wave][u + i][p.lane] = {gx, gd};
                     const float r = reduce8(v, p.lane);
-                    const int j = p.lane >> 3;
-                    if ((p.lane & 7) == 0) sbc[(k * 2 + (j >> 2)) * sp + p.wave * kSL + (j & 3)] = r;
+                    if ((p.lane & 7) == 0) m.sgbc[u + i][p.wave][p.lane >> 3] = r;
+                }
+                __builtin_amdgcn_sched_barrier(0);
+                if (u > 0) {
+#pragma unroll
+                    for (int i = 0; i < U; ++i) step[i] = ahead[i];
                 }
             }
+#pragma unroll
+            for (int s = 0; s < kSL; ++s) h[s] = h_next[s];
         }
-        __syncthreads();
-        for (int k = p.wave; k < K && t0 + k < a.T; k += waves) {
-            float gx = 0.0f, gdt = 0.0f;
-            if (k < n) {
-                const f32x4_t d = sd[k * kWave + p.lane];
-                float db = 0.0f, da = 0.0f;
-                for (int w = 0; w < waves; ++w) {
-                    const float2 g = sg[(w * K + k) * kWave + p.lane];
-                    db += g.x;
-                    da += g.y;
+        lds_barrier();
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+            const int k = p.wave + r * NS;
+            if (k < K && t0 + k < p.t1) {
+                float gx = 0.0f, gdt = 0.0f;
+                if (t0 + k < p.len) {
+                    const Step s = m.sd[buf][k][p.lane];
+                    float db = 0.0f, da = 0.0f;
+                    for (int w = 0; w < used; ++w) {
+                        const float2 g = m.sg[w][k][p.lane];
+                        db += g.x;
+                        da += g.y;
+                    }
+                    gx = fmaf(s.d, db, skip * s.gy);
+                    const float x = IoVec<IO, 1>::get(own[r].x, 0);
+                    gdt = fmaf(x, db, da * kLn2);                // rate is A log2 e
+                    if (a.softplus) gdt *= sigmoid(IoVec<IO, 1>::get(own[r].dt, 0) + bias);
+                    gD = fmaf(s.gy, x, gD);
+                    gbias += gdt;
                 }
-                gx = fmaf(d[0], db, skip * d[2]);
-                gdt = fmaf(d[3], db, da * kLn2);                 // rate is A log2 e
-                if (a.softplus) gdt *= sigmoid(load1<IO>(at<IO>(a.dt, t0 + k, p.b, p.f)) + bias);
-                gD = fmaf(d[2], d[3], gD);
-                gbias += gdt;
+                if (p.active) {
+                    cgx.store(t0 + k, gx);
+                    cgdt.store(t0 + k, gdt);
+                }
             }
-            if (p.active) {
-                store1<IO>(at_out<IO>(a.gx, t0 + k, p.b, p.f), gx);
-                store1<IO>(at_out<IO>(a.gdt, t0 + k, p.b, p.f), gdt);
+            own[r] = staged[r];
+        }
+        {
+            const int64_t row = int64_t(a.B) * a.G * (NS * 2 * kSL);
+            float* part = a.part_bc + p.tile * a.T * row + (p.b * a.G + p.g) * (NS * 2 * kSL);
+            for (int i = threadIdx.x; i < K * NS * 2 * kSL; i += NS * kWave) {
+                const int k = i / (NS * 2 * kSL), j = i % (NS * 2 * kSL);
+                if (t0 + k < p.len) part[(t0 + k) * row + j] = m.sgbc[k][0][j];
             }
         }
-        for (int i = threadIdx.x; i < K * 2 * sp; i += waves * kWave) {
-            const int k = i / (2 * sp), s = i - k * 2 * sp;
-            if (t0 + k < a.T) part[((t0 + k) * a.B + p.b) * row + p.g * 2 * sp + s] = k < n ? sbc[i] : 0.0f;
-        }
-        __syncthreads();
+        lds_barrier();
+        buf ^= 1;
     }
-    if (a.gh_in != nullptr) store_state(a, p, a.gh_in, e);
-    float* pf = a.part_f + p.b * (a.F * (a.S + 2));
-    store_state(a, {p.lane, p.wave, p.g, p.tile, 0, p.f, p.active}, pf, gA);
-    float* s2 = lds;                                             // [waves][2][64]
-    s2[(p.wave * 2) * kWave + p.lane] = gD;
-    s2[(p.wave * 2 + 1) * kWave + p.lane] = gbias;
-    __syncthreads();
+    if (a.gh_in != nullptr && p.t0 == 0) store_state(a, p, a.gh_in, e);
+    float* pf = a.part_f + p.b * scan_partial_values(a.F, a.S);
+#pragma unroll
+    for (int i = 0; i < kSL; ++i)
+        if (p.active && i < p.states) pf[p.f * a.S + p.first + i] = gA[i];
+    m.sg[p.wave][0][p.lane] = {gD, gbias};
+    lds_barrier();
     if (p.wave == 0 && p.active) {
-        float sum[2] = {0.0f, 0.0f};
-        for (int w = 0; w < waves; ++w) {
-            sum[0] += s2[(w * 2) * kWave + p.lane];
-            sum[1] += s2[(w * 2 + 1) * kWave + p.lane];
+        float2 sum = {0.0f, 0.0f};
+        for (int w = 0; w < NS; ++w) {
+            sum.x += m.sg[w][0][p.lane].x;
+            sum.y += m.sg[w][0][p.lane].y;
         }
-        pf[a.F * a.S + p.f] = sum[0];
-        pf[a.F * (a.S + 1) + p.f] = sum[1];
+        pf[a.F * a.S + p.f] = sum.x;
+        pf[a.F * (a.S + 1) + p.f] = sum.y;
     }
 }
 
@@ -171,35 +258,49 @@ template <int IO>
 __global__ __launch_bounds__(kBlock) void scan_join_kernel(ScanArgs a, int64_t n) {
     const int64_t i = int64_t(blockIdx.x) * kBlock + threadIdx.x;
     if (i >= n) return;
-    const int s = int(i % a.S);
+    const int waves = a.plan.waves, s = int(i % a.S);
     const int64_t q = i / a.S, which = q & 1, r = q >> 1;
     const int64_t g = r % a.G, tb = r / a.G, b = tb % a.B, t = tb / a.B;
-    const int64_t stride = a.T * a.B * a.G * 2 * a.plan.sp;
-    const float* part = a.part_bc + (r * 2 + which) * a.plan.sp + s;
     float sum = 0.0f;
-    for (int64_t j = 0; j < a.plan.tiles; ++j) sum += part[j * stride];
+    if (t < steps_of(a.lengths, b, a.T)) {
+        const int64_t stride = a.T * a.B * a.G * waves * 2 * kSL;
+        const float* part = a.part_bc + (r * waves + s / kSL) * 2 * kSL + which * kSL + s % kSL;
+        for (int64_t j = 0; j < a.plan.tiles; ++j) sum += part[j * stride];
+    }
     store1<IO>(at_out<IO>(which ? a.gC : a.gB, t, b, g * a.S + s), sum);
 }
 
-template <int IO, int K>
+template <int IO, int NS>
 snn_status backward_launch(const ScanArgs& a, hipStream_t s) {
-    const int lds = K * 4 * (kWave * (4 + 2 * a.plan.waves) + 2 * a.plan.sp);
-    hipLaunchKernelGGL((scan_backward_kernel<IO, K>), dim3(unsigned(a.plan.tiles * a.G * a.B)), dim3(a.plan.waves * kWave),
-                       lds, s, a);
-    if (hipGetLastError() != hipSuccess) return SNN_E_LAUNCH;
-    const int64_t n = a.T * a.B * a.G * 2 * a.S;
-    snn_status st = launch(scan_join_kernel<IO>, grid_for(n), s, a, n);
+    ScanArgs arg = a;
+    void* argv[] = {&arg};
+    const dim3 grid(unsigned(a.plan.tiles * a.G * a.B), unsigned(a.plan.segments));
+    const hipError_t e = hipLaunchKernel(reinterpret_cast<const void*>(scan_backward_kernel<IO, NS>), grid,
+                                         dim3(NS * kWave), argv, sizeof(BackwardLds<NS>), s);
+    return e == hipSuccess ? SNN_OK : SNN_E_LAUNCH;
+}
+
+template <int IO>
+snn_status backward_io(const ScanArgs& a, hipStream_t s) {
+    snn_status st;
+    switch (a.plan.waves) {
+        case 1: st = backward_launch<IO, 1>(a, s); break;
+        case 2: st = backward_launch<IO, 2>(a, s); break;
+        case 4: st = backward_launch<IO, 4>(a, s); break;
+        case 8: st = backward_launch<IO, 8>(a, s); break;
+        default: st = backward_launch<IO, 16>(a, s); break;
+    }
     if (st != SNN_OK) return st;
+    const int64_t n = a.T * a.B * a.G * 2 * a.S;
+    if ((st = launch(scan_join_kernel<IO>, grid_for(n), s, a, n)) != SNN_OK) return st;
     const ReduceOut out = {{a.gA, a.gD, a.gdt_bias}, {a.F * a.S, a.F, a.F}};
-    return reduce_entry(a.part_f, a.B, scan_partial_values(a.F, a.S), out, s);
+    return reduce_entry(a.part_f, a.plan.segments * a.B, scan_partial_values(a.F, a.S), out, s);
 }
 
 }  // namespace
 
 snn_status scan_backward_entry(int io, const ScanArgs& a, hipStream_t s) {
-    if (a.plan.k == 16)
-        return io == SNN_IO_F32 ? backward_launch<SNN_IO_F32, 16>(a, s) : backward_launch<SNN_IO_BF16, 16>(a, s);
-    return io == SNN_IO_F32 ? backward_launch<SNN_IO_F32, 8>(a, s) : backward_launch<SNN_IO_BF16, 8>(a, s);
+    return io == SNN_IO_F32 ? backward_io<SNN_IO_F32>(a, s) : backward_io<SNN_IO_BF16>(a, s);
 }
 
 }  // namespace snnlif

@@ -1,104 +1,149 @@
 // Selective state space scan, forward.
 //
 // Per step, feature and state: a = 2^(d A log2 e), h = a h + (d x) B, y += C h: five vector
-// instructions, one of them an exponential.  With S = 16 states that is more work than the
-// few bytes per feature and step need to move, so the kernel is bound by the vector ALU.
-// A lane is a feature, each wave of a workgroup holds 4 of its states in registers, and B and
-// C come through scalar registers.  What belongs to a step but not to a state (the softplus,
-// the sum of y over the waves) is shared out over the waves, K steps at a time, through LDS.
+// instructions, one of them an exponential at half rate.  With S = 16 states that is more
+// work than the few bytes per feature and step need to move, so the kernel is bound by the
+// vector ALU.  A lane is a feature and each wave of a workgroup holds 4 of its states in
+// registers.  What belongs to a step but not to a state (the softplus, B and C, the sum of y
+// over the waves) is shared out over the waves, K steps at a time, through LDS: while a
+// block's steps run, the one after the next is staged and the third is loaded, and one
+// barrier parts two blocks.
 #include "seq_scan.h"
 
 namespace snnlif {
 namespace {
 
-template <int IO>
-__global__ __launch_bounds__(kBlock) void scan_pack_kernel(ScanArgs a, int64_t n) {
-    const int64_t i = int64_t(blockIdx.x) * kBlock + threadIdx.x;
-    if (i >= n) return;
-    const int sp = a.plan.sp;
-    const int s = int(i % sp);
-    const int64_t q = i / sp, which = q & 1, r = q >> 1;     // r = (t B + b) G + g
-    const int64_t g = r % a.G, tb = r / a.G, b = tb % a.B, t = tb / a.B;
-    a.packed[i] = s < a.S ? load1<IO>(at<IO>(which ? a.Cm : a.Bm, t, b, g * a.S + s)) : 0.0f;
-}
-
-template <int IO, int K>
-__global__ __launch_bounds__(1024) void scan_forward_kernel(ScanArgs a) {
-    extern __shared__ float lds[];
+template <int IO, int NS>
+__global__ __launch_bounds__(NS * kWave) void scan_forward_kernel(ScanArgs a) {
+    constexpr int K = kScanBlock, R = K > NS ? K / NS : 1, U = 2;   // U: steps read from LDS ahead
+    __shared__ float2 sd[3][K][kWave];           // (d, d x): of this block, the next and the one being staged
+    __shared__ float sy[2][NS][K][kWave];
+    __shared__ __align__(16) StagedBC<NS, K> sbc[3];
     const ScanPlace p = scan_place(a);
-    const int waves = a.plan.waves;
-    float2* sd = reinterpret_cast<float2*>(lds);                 // [K][64] (d, d x)
-    float* sy = lds + K * kWave * 2;                             // [waves][K][64]
     float rate[kSL], h[kSL];
     load_rates(a, p, rate);
     load_state(a, p, a.h_in, h);
     const float skip = a.D != nullptr ? a.D[p.f] : 0.0f, bias = a.dt_bias != nullptr ? a.dt_bias[p.f] : 0.0f;
-    const int64_t len = steps_of(a.lengths, p.b, a.T);
-    const int64_t row = int64_t(a.G) * 2 * a.plan.sp;            // packed values per (t, b)
+    const Column<IO> cx(a.x, p), cdt(a.dt, p), cy(a.y, p);
+    BCColumns<IO, NS, K> cbc(a, p);
+    const StateColumn kept(a, p, a.saved);
+    const bool busy = p.states > 0;              // waves behind the last state only share the rest
+    const int used = (a.S + kSL - 1) / kSL;
 
-    for (int64_t c = 0; c < a.plan.blocks; ++c) {
-        const int64_t t0 = c * K;
-        if (c > 0 && a.saved != nullptr && t0 < len) {
+    typename IoVec<IO, 1>::raw xr[R], dr[R];
+    float xs[3][R];                              // D x of this wave's steps
+    const auto fetch = [&](int t0) {
+        cbc.fetch(t0, p.len);
 #pragma unroll
-            for (int i = 0; i < kSL; ++i)
-                if (p.active && p.wave * kSL + i < a.S) a.saved[kept_at(a, p, c, p.wave * kSL + i)] = h[i];
+        for (int r = 0; r < R; ++r) {
+            const int k = p.wave + r * NS;
+            if (k < K && t0 + k < p.len) {
+                xr[r] = cx.load(t0 + k);
+                dr[r] = cdt.load(t0 + k);
+            }
         }
-        for (int k = p.wave; k < K; k += waves) {
-            float2 d = {0.0f, 0.0f};
-            if (t0 + k < len) {
-                const float v = load1<IO>(at<IO>(a.dt, t0 + k, p.b, p.f)) + bias;
+    };
+    const auto stage = [&](int t0, int to, float (&skipped)[R]) {
+        cbc.stage(t0, p.len, sbc[to]);
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+            const int k = p.wave + r * NS;
+            float2 d = {0.0f, 0.0f};             // behind the end: the state stays
+            skipped[r] = 0.0f;
+            if (k < K && t0 + k < p.len) {
+                const float v = IoVec<IO, 1>::get(dr[r], 0) + bias, x = IoVec<IO, 1>::get(xr[r], 0);
                 d.x = a.softplus ? softplus(v) : v;
-                d.y = d.x * load1<IO>(at<IO>(a.x, t0 + k, p.b, p.f));
+                d.y = d.x * x;
+                skipped[r] = skip * x;
             }
-            sd[k * kWave + p.lane] = d;
+            if (k < K) sd[to][k][p.lane] = d;
         }
-        __syncthreads();
-        const int64_t n = min(int64_t(K), len - t0);
-        for (int k = 0; k < n; ++k) {
-            const float2 d = sd[k * kWave + p.lane];
-            const float* bc = a.packed + ((t0 + k) * a.B + p.b) * row + p.g * 2 * a.plan.sp + p.wave * kSL;
-            const f32x4_t bv = scalar_load4(bc), cv = scalar_load4(bc + a.plan.sp);
-            float y = 0.0f;
+    };
+
+    fetch(p.t0);
+    stage(p.t0, 0, xs[0]);
+    fetch(p.t0 + K);
+    stage(p.t0 + K, 1, xs[1]);
+    fetch(p.t0 + 2 * K);
+    struct Step {
+        float2 d;
+        f32x4_t b, c;
+    } step[U], ahead[U];
+    const auto read = [&](int block, int k) {
+        const f32x4_t* bc = reinterpret_cast<const f32x4_t*>(sbc[block].v[k][p.wave]);
+        return Step{sd[block][k][p.lane], bc[0], bc[1]};
+    };
+    lds_barrier();
 #pragma unroll
-            for (int i = 0; i < kSL; ++i) {
-                h[i] = fmaf(__builtin_amdgcn_exp2f(d.x * rate[i]), h[i], d.y * bv[i]);
-                y = fmaf(cv[i], h[i], y);
+    for (int i = 0; i < U; ++i) step[i] = read(0, i);
+    int now = 0, buf = 0;                        // block c: c % 3 and c % 2
+    for (int t0 = p.t0; t0 < p.t1; t0 += K) {
+        const int next = now == 2 ? 0 : now + 1, last = now == 0 ? 2 : now - 1;
+        if (t0 < p.len) {
+            if (a.saved != nullptr && t0 > 0 && (t0 & (a.plan.keep - 1)) == 0)
+                if (busy && p.active) kept.store(t0 / a.plan.keep - 1, h);
+            stage(t0 + 2 * K, last, xs[2]);
+            fetch(t0 + 3 * K);
+            if (busy) {
+#pragma unroll
+                for (int u = 0; u < K; u += U) {
+#pragma unroll
+                    for (int i = 0; i < U; ++i)
+                        ahead[i] = u + U < K ? read(now, u + U + i) : read(next, u + U - K + i);
+                    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+                    for (int i = 0; i < U; ++i) {
+                        float y = 0.0f;
+#pragma unroll
+                        for (int s = 0; s < kSL; ++s) {
+                            h[s] = fmaf(__builtin_amdgcn_exp2f(step[i].d.x * rate[s]), h[s], step[i].d.y * step[i].b[s]);
+                            y = fmaf(step[i].c[s], h[s], y);
+                        }
+                        sy[buf][p.wave][u + i][p.lane] = y;
+                    }
+                    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+                    for (int i = 0; i < U; ++i) step[i] = ahead[i];
+                }
             }
-            sy[(p.wave * K + k) * kWave + p.lane] = y;
         }
-        __syncthreads();
-        for (int k = p.wave; k < K && t0 + k < a.T; k += waves) {
-            float y = 0.0f;
-            if (t0 + k < len) {
-                y = skip * load1<IO>(at<IO>(a.x, t0 + k, p.b, p.f));
-                for (int w = 0; w < waves; ++w) y += sy[(w * K + k) * kWave + p.lane];
+        lds_barrier();
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+            const int k = p.wave + r * NS;
+            if (k < K && t0 + k < p.t1) {
+                float y = 0.0f;
+                if (t0 + k < p.len) {
+                    y = xs[0][r];
+                    for (int w = 0; w < used; ++w) y += sy[buf][w][k][p.lane];
+                }
+                if (p.active) cy.store(t0 + k, y);
             }
-            if (p.active) store1<IO>(at_out<IO>(a.y, t0 + k, p.b, p.f), y);
+            xs[0][r] = xs[1][r];
+            xs[1][r] = xs[2][r];
         }
+        now = next;
+        buf ^= 1;
     }
-    if (a.h_out != nullptr) store_state(a, p, a.h_out, h);
+    if (a.h_out != nullptr && p.t1 == a.T) store_state(a, p, a.h_out, h);
 }
 
-template <int IO, int K>
-snn_status forward_launch(const ScanArgs& a, hipStream_t s) {
-    const int lds = K * kWave * 4 * (2 + a.plan.waves);
-    hipLaunchKernelGGL((scan_forward_kernel<IO, K>), dim3(unsigned(a.plan.tiles * a.G * a.B)), dim3(a.plan.waves * kWave),
-                       lds, s, a);
-    return hipGetLastError() == hipSuccess ? SNN_OK : SNN_E_LAUNCH;
+template <int IO>
+snn_status forward_io(const ScanArgs& a, hipStream_t s) {
+    const dim3 grid(unsigned(a.plan.tiles * a.G * a.B), unsigned(a.plan.segments));
+    switch (a.plan.waves) {
+        case 1: return launch_blk(scan_forward_kernel<IO, 1>, grid, 1 * kWave, s, a);
+        case 2: return launch_blk(scan_forward_kernel<IO, 2>, grid, 2 * kWave, s, a);
+        case 4: return launch_blk(scan_forward_kernel<IO, 4>, grid, 4 * kWave, s, a);
+        case 8: return launch_blk(scan_forward_kernel<IO, 8>, grid, 8 * kWave, s, a);
+        default: return launch_blk(scan_forward_kernel<IO, 16>, grid, 16 * kWave, s, a);
+    }
 }
 
 }  // namespace
 
-snn_status scan_pack_entry(int io, const ScanArgs& a, hipStream_t s) {
-    const int64_t n = a.T * a.B * a.G * 2 * a.plan.sp;
-    return io == SNN_IO_F32 ? launch(scan_pack_kernel<SNN_IO_F32>, grid_for(n), s, a, n)
-                            : launch(scan_pack_kernel<SNN_IO_BF16>, grid_for(n), s, a, n);
-}
-
 snn_status scan_forward_entry(int io, const ScanArgs& a, hipStream_t s) {
-    if (a.plan.k == 16)
-        return io == SNN_IO_F32 ? forward_launch<SNN_IO_F32, 16>(a, s) : forward_launch<SNN_IO_BF16, 16>(a, s);
-    return io == SNN_IO_F32 ? forward_launch<SNN_IO_F32, 8>(a, s) : forward_launch<SNN_IO_BF16, 8>(a, s);
+    return io == SNN_IO_F32 ? forward_io<SNN_IO_F32>(a, s) : forward_io<SNN_IO_BF16>(a, s);
 }
 
 }  // namespace snnlif

@@ -34,9 +34,9 @@ snn_status check_scan(const snn_scan_cfg* c, int64_t T, int64_t B, int64_t F) {
     if (check_seq_shape(T, B, F) != SNN_OK) return SNN_E_SHAPE;
     if (F % c->groups != 0) return SNN_E_SHAPE;
     if (empty(T, B, F)) return SNN_OK;
-    const ScanPlan p = scan_plan(c, T, F);
+    const ScanPlan p = scan_plan(c, T, B, F);
     if (p.tiles * c->groups > kMaxBlocks / B) return SNN_E_SHAPE;
-    return scan_packed(c, p, T, B) / 4 <= kMaxBlocks * kBlock && F * c->states <= kMaxSpan / B ? SNN_OK : SNN_E_SHAPE;
+    return T * B * c->groups <= kMaxBlocks && F * c->states <= kMaxSpan / B ? SNN_OK : SNN_E_SHAPE;
 }
 
 snn_status check_norm(const snn_norm_cfg* c, int64_t T, int64_t B, int64_t F) {
@@ -65,7 +65,7 @@ ScanArgs scan_args(const snn_scan_cfg* c, int64_t T, int64_t B, int64_t F, const
     a.dt_bias = dt_bias;
     a.h_in = h_in;
     a.lengths = lengths;
-    a.plan = scan_plan(c, T, F);
+    a.plan = scan_plan(c, T, B, F);
     return a;
 }
 
@@ -204,8 +204,6 @@ snn_status snn_scan_forward(const snn_scan_cfg* cfg, int64_t T, int64_t B, int64
     a.y = rows(y);
     a.h_out = h_out;
     a.saved = static_cast<float*>(saved);
-    a.packed = static_cast<float*>(workspace);
-    if ((st = scan_pack_entry(cfg->io, a, stream_of(stream))) != SNN_OK) return st;
     return scan_forward_entry(cfg->io, a, stream_of(stream));
 }
 
@@ -238,12 +236,9 @@ snn_status snn_scan_backward(const snn_scan_cfg* cfg, int64_t T, int64_t B, int6
     a.gD = grad_D;
     a.gdt_bias = grad_dt_bias;
     a.gh_in = grad_h_in;
-    const int64_t packed = scan_packed(cfg, a.plan, T, B);
     int64_t at = 0;
-    a.packed = carve<float>(workspace, at, packed);
-    a.part_bc = carve<float>(workspace, at, packed * a.plan.tiles);
+    a.part_bc = carve<float>(workspace, at, scan_partial_bc(cfg, a.plan, T, B));
     a.part_f = carve<float>(workspace, at, B * scan_partial_values(F, cfg->states) * 4);
-    if ((st = scan_pack_entry(io, a, stream_of(stream))) != SNN_OK) return st;
     return scan_backward_entry(io, a, stream_of(stream));
 }
 
