@@ -17,7 +17,7 @@ T* carve(void* base, int64_t& at, int64_t bytes) {
 }
 
 // Workspace: NULL only where its size is 0.  Pieces of it start on boundaries of their own.
-snn_status check_workspace(const void* ws, int64_t bytes) { return bytes == 0 ? SNN_OK : need(ws, 16); }
+snn_status check_workspace(const void* ws, int64_t bytes) { return bytes == 0 ? optional(ws, 16) : need(ws, 16); }
 
 snn_status check_conv(const snn_conv_cfg* c, int64_t T, int64_t B, int64_t F) {
     const snn_status st = check_conv_cfg(c);

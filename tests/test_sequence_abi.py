@@ -79,8 +79,8 @@ def test_null_arguments(name):
     assert call(name, cfg=None) == -1
     for k in CALLS[name]:
         if k not in OPTIONAL and k != "cfg":
-            if k == "saved" and name == "snn_scan_forward" or k == "rstd" and name == "snn_norm_forward":
-                continue
+            if name == "snn_scan_forward" and k in ("saved", "workspace") or name == "snn_norm_forward" and k == "rstd":
+                continue         # not needed, or not for few steps
             if k == "saved":     # needed as soon as there are two blocks of steps
                 assert call(name, (40, 3, 20), **{k: None}) == -1
                 continue
