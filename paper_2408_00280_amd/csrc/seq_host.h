@@ -208,10 +208,20 @@ inline snn_status check_norm_cfg(const snn_norm_cfg* c) {
     return check_io(c->io) == SNN_OK && c->eps > 0.0f && std::isfinite(c->eps) ? SNN_OK : SNN_E_PARAM;
 }
 
-// Workgroups of the backward; each walks rows g, g + groups, ... and keeps one partial sum of
-// the parameters' gradients.
-inline int64_t norm_groups(int64_t T, int64_t B) { return std::min<int64_t>(T * B, 1024); }
-inline int64_t norm_workspace(int64_t T, int64_t B, int64_t F) { return piece(norm_groups(T, B) * 3 * F * 4); }
+// Rows of up to 8192 features stay in registers, 8 features per lane; longer ones are read
+// again for each sum, by workgroups of kBlock lanes.
+constexpr int kNormLane = 8, kNormRegs = 1024 * kNormLane;
+
+inline int norm_lanes(int64_t F) {
+    return F > kNormRegs ? kBlock : int(ceil_div(F, kNormLane * kWave) * kWave);
+}
+
+// Workgroups walk rows g, g + groups, ...: parameters are read once and the backward keeps
+// one partial sum of their gradients.  16 waves per CU hide the latency of the sums.
+inline int64_t norm_groups(int64_t T, int64_t B, int64_t F) {
+    return std::min<int64_t>(T * B, ceil_div(256 * 16, norm_lanes(F) / kWave));
+}
+inline int64_t norm_workspace(int64_t T, int64_t B, int64_t F) { return piece(norm_groups(T, B, F) * 3 * F * 4); }
 
 struct NormArgs {
     int64_t T, B, F;

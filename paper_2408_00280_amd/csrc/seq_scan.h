@@ -125,11 +125,4 @@ struct BCColumns {
     }
 };
 
-// A barrier that orders the LDS only: loads from memory stay in flight over it.
-__device__ __forceinline__ void lds_barrier() {
-    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup", "local");
-    __builtin_amdgcn_s_barrier();
-    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
-}
-
 }  // namespace snnlif

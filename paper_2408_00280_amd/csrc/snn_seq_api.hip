@@ -93,7 +93,7 @@ NormArgs norm_args(const snn_norm_cfg* c, int64_t T, int64_t B, int64_t F, const
     a.scale = scale;
     a.w_pre = w_pre;
     a.lengths = lengths;
-    a.groups = norm_groups(T, B);
+    a.groups = norm_groups(T, B, F);
     return a;
 }
 
