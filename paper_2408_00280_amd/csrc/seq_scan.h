@@ -74,15 +74,18 @@ struct StateColumn {
     }
 };
 
-// A lane's column of a [T][B][F] tensor.
+// The lanes' columns of a [T][B][F] tensor: a row's address is the same for the whole wave and
+// stays in scalar registers, a lane adds the offset of its feature.
 template <int IO>
-struct Column {
+struct Columns {
     static constexpr int kBytes = IO == SNN_IO_F32 ? 4 : 2;
-    const char* p;
+    const char* base;
     int64_t step;    // bytes
-    __device__ Column(const Rows& r, const ScanPlace& s) : p(static_cast<const char*>(at<IO>(r, 0, s.b, s.f))), step(r.t * kBytes) {}
-    __device__ auto load(int t) const { return IoVec<IO, 1>::load(p + t * step, 0); }
-    __device__ void store(int t, float v) const { store1<IO>(const_cast<char*>(p) + t * step, v); }
+    unsigned lane;   // bytes
+    __device__ Columns(const Rows& r, const ScanPlace& s)
+        : base(static_cast<const char*>(r.p) + s.b * r.b * kBytes), step(r.t * kBytes), lane(unsigned(s.f) * kBytes) {}
+    __device__ auto load(int t) const { return IoVec<IO, 1>::load(base + t * step + lane, 0); }
+    __device__ void store(int t, float v) const { store1<IO>(const_cast<char*>(base + t * step + lane), v); }
 };
 
 // B and C of one step and group are the same for every lane of a wave.  Each block of steps is
@@ -99,23 +102,26 @@ struct StagedBC {
 template <int IO, int NS, int K>
 struct BCColumns {
     static constexpr int N = StagedBC<NS, K>::N, kApart = kWave / (2 * kSL);   // steps between a thread's values
-    const char* p;
+    const char* p;       // of the next block to fetch
     int64_t step;
     int k;
     bool in;
     typename IoVec<IO, 1>::raw raw[N];
-    __device__ BCColumns(const ScanArgs& a, const ScanPlace& s) {
+    __device__ BCColumns(const ScanArgs& a, const ScanPlace& s, int t0) {
         const int j = threadIdx.x % (NS * 2 * kSL), n = j / (2 * kSL) * kSL + j % kSL;
         const Rows& r = (j & kSL) ? a.Cm : a.Bm;
         k = threadIdx.x / (NS * 2 * kSL);
         in = n < a.S;
         step = r.t * (IO == SNN_IO_F32 ? 4 : 2);
-        p = static_cast<const char*>(at<IO>(r, k, s.b, s.g * a.S + (in ? n : 0)));
+        p = static_cast<const char*>(at<IO>(r, t0 + k, s.b, s.g * a.S + (in ? n : 0)));
     }
-    __device__ void fetch(int t0, int len) {
+    // Blocks one after the other, up (DIR = 1) or down the time axis.
+    template <int DIR>
+    __device__ void fetch(int t0, int first, int len) {
 #pragma unroll
         for (int i = 0; i < N; ++i)
-            if (in && t0 + k + i * kApart < len) raw[i] = IoVec<IO, 1>::load(p + (t0 + i * kApart) * step, 0);
+            if (in && t0 >= first && t0 + k + i * kApart < len) raw[i] = IoVec<IO, 1>::load(p + i * kApart * step, 0);
+        p += DIR * K * step;
     }
     __device__ void stage(int t0, int len, StagedBC<NS, K>& to) const {
 #pragma unroll

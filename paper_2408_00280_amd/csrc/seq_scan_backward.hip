@@ -63,8 +63,7 @@ __global__ __launch_bounds__(NS * kWave, NS > 8 ? 4 : 2) void scan_backward_kern
 #pragma unroll
     for (int i = 0; i < kSL; ++i) gA[i] = 0.0f;
     const float skip = a.D != nullptr ? a.D[p.f] : 0.0f, bias = a.dt_bias != nullptr ? a.dt_bias[p.f] : 0.0f;
-    const Column<IO> cx(a.x, p), cdt(a.dt, p), cgy(a.gy, p), cgx(a.gx, p), cgdt(a.gdt, p);
-    BCColumns<IO, NS, K> cbc(a, p);
+    const Columns<IO> cx(a.x, p), cdt(a.dt, p), cgy(a.gy, p), cgx(a.gx, p), cgdt(a.gdt, p);
     const bool busy = p.states > 0;
     const int used = (a.S + kSL - 1) / kSL;
 
@@ -72,16 +71,14 @@ __global__ __launch_bounds__(NS * kWave, NS > 8 ? 4 : 2) void scan_backward_kern
         typename IoVec<IO, 1>::raw x, dt, gy;
     };
     Raw raw[R], own[R];          // of the next block; of this block, for its end
-    const auto fetch = [&](int t0) {
-        if (t0 >= p.t0) cbc.fetch(t0, p.len);
+    const auto fetch_rows = [&](int t0) {
 #pragma unroll
         for (int r = 0; r < R; ++r) {
             const int k = p.wave + r * NS;
             if (k < K && t0 >= p.t0 && t0 + k < p.len) raw[r] = {cx.load(t0 + k), cdt.load(t0 + k), cgy.load(t0 + k)};
         }
     };
-    const auto stage = [&](int t0, int to) {
-        if (t0 >= p.t0) cbc.stage(t0, p.len, m.sbc[to]);
+    const auto stage_rows = [&](int t0, int to) {
 #pragma unroll
         for (int r = 0; r < R; ++r) {
             const int k = p.wave + r * NS;
@@ -108,6 +105,15 @@ __global__ __launch_bounds__(NS * kWave, NS > 8 ? 4 : 2) void scan_backward_kern
             }
         }
     }
+    BCColumns<IO, NS, K> cbc(a, p, t0);
+    const auto fetch = [&](int t0) {
+        cbc.template fetch<-1>(t0, p.t0, p.len);
+        fetch_rows(t0);
+    };
+    const auto stage = [&](int t0, int to) {
+        if (t0 >= p.t0) cbc.stage(t0, p.len, m.sbc[to]);
+        stage_rows(t0, to);
+    };
     fetch(t0);
     stage(t0, 0);
 #pragma unroll
@@ -204,11 +210,14 @@ __global__ __launch_bounds__(NS * kWave, NS > 8 ? 4 : 2) void scan_backward_kern
                 float gx = 0.0f, gdt = 0.0f;
                 if (t0 + k < p.len) {
                     const Step s = m.sd[buf][k][p.lane];
+                    float2 g[NS];
                     float db = 0.0f, da = 0.0f;
-                    for (int w = 0; w < used; ++w) {
-                        const float2 g = m.sg[w][k][p.lane];
-                        db += g.x;
-                        da += g.y;
+#pragma unroll
+                    for (int w = 0; w < NS; ++w) g[w] = m.sg[w][k][p.lane];
+#pragma unroll
+                    for (int w = 0; w < NS; ++w) {
+                        db += w < used ? g[w].x : 0.0f;
+                        da += w < used ? g[w].y : 0.0f;
                     }
                     gx = fmaf(s.d, db, skip * s.gy);
                     const float x = IoVec<IO, 1>::get(own[r].x, 0);

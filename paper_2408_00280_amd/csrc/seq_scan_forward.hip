@@ -24,8 +24,8 @@ __global__ __launch_bounds__(NS * kWave) void scan_forward_kernel(ScanArgs a) {
     load_rates(a, p, rate);
     load_state(a, p, a.h_in, h);
     const float skip = a.D != nullptr ? a.D[p.f] : 0.0f, bias = a.dt_bias != nullptr ? a.dt_bias[p.f] : 0.0f;
-    const Column<IO> cx(a.x, p), cdt(a.dt, p), cy(a.y, p);
-    BCColumns<IO, NS, K> cbc(a, p);
+    const Columns<IO> cx(a.x, p), cdt(a.dt, p), cy(a.y, p);
+    BCColumns<IO, NS, K> cbc(a, p, p.t0);
     const StateColumn kept(a, p, a.saved);
     const bool busy = p.states > 0;              // waves behind the last state only share the rest
     const int used = (a.S + kSL - 1) / kSL;
@@ -33,7 +33,7 @@ __global__ __launch_bounds__(NS * kWave) void scan_forward_kernel(ScanArgs a) {
     typename IoVec<IO, 1>::raw xr[R], dr[R];
     float xs[3][R];                              // D x of this wave's steps
     const auto fetch = [&](int t0) {
-        cbc.fetch(t0, p.len);
+        cbc.template fetch<1>(t0, p.t0, p.len);
 #pragma unroll
         for (int r = 0; r < R; ++r) {
             const int k = p.wave + r * NS;
@@ -114,8 +114,12 @@ __global__ __launch_bounds__(NS * kWave) void scan_forward_kernel(ScanArgs a) {
             if (k < K && t0 + k < p.t1) {
                 float y = 0.0f;
                 if (t0 + k < p.len) {
+                    float part[NS];
+#pragma unroll
+                    for (int w = 0; w < NS; ++w) part[w] = sy[buf][w][k][p.lane];
                     y = xs[0][r];
-                    for (int w = 0; w < used; ++w) y += sy[buf][w][k][p.lane];
+#pragma unroll
+                    for (int w = 0; w < NS; ++w) y += w < used ? part[w] : 0.0f;
                 }
                 if (p.active) cy.store(t0 + k, y);
             }
