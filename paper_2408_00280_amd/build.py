@@ -38,8 +38,8 @@ UNITS = (
        for io in (0, 1) for spk in (0, 1, 2)]
     + [(f"stackb_io{io}", "lif_stack.hip", [f"-DSNNLIF_IO={io}", "-DSNNLIF_STACK_BWD=1"]) for io in (0, 1)]
     + [("glue", "lif_glue.hip", []), ("serial", "lif_serial.hip", []), ("api", "snn_lif_api.hip", [])]
-    + [(name, f"{name}.hip", []) for name in ("seq_conv", "seq_scan_forward", "seq_scan_backward", "seq_norm",
-                                              "snn_seq_api")]
+    + [(name, f"{name}.hip", []) for name in ("seq_conv", "seq_scan_forward", "seq_scan_backward", "seq_scan_split",
+                                              "seq_norm", "snn_seq_api")]
 )
 
 

@@ -145,6 +145,7 @@ inline snn_status check_scan_cfg(const snn_scan_cfg* c) {
 
 constexpr int kScanStates = 4;   // states per lane
 constexpr int kScanBlock = 8;    // steps that the waves share out at a time
+constexpr int64_t kSplitWaves = 1024, kMaxSegments = 1024;
 
 // A workgroup owns 64 features of one group and one sequence, a feature per lane; each of its
 // `waves` (a power of two) waves holds 4 of their states.  The forward keeps the state every
@@ -160,29 +161,50 @@ struct ScanPlan {
 
 constexpr int scan_keep(int waves) { return waves == 4 || waves == 8 ? 16 : 8; }
 
+// States as they are kept: whole lanes.
+constexpr int64_t scan_held_states(int S) { return int64_t(S + kScanStates - 1) / kScanStates * kScanStates; }
+
+// The time axis is cut into segments where the waves of one segment leave SIMDs (1024 of them)
+// without two waves: the local pass then costs less than the idle SIMDs.  Four waves per SIMD
+// are aimed for, and segments of 64 steps or more.
 inline ScanPlan scan_plan(const snn_scan_cfg* c, int64_t T, int64_t B, int64_t F) {
     ScanPlan p;
     p.waves = 1;
     while (p.waves * kScanStates < c->states) p.waves *= 2;
     p.keep = scan_keep(p.waves);
     p.tiles = ceil_div(F / c->groups, kWave);
+    p.steps = std::max<int64_t>(T, 1);
     p.segments = 1;
-    p.steps = T;
+    const int64_t waves = p.tiles * c->groups * B * (scan_held_states(c->states) / kScanStates);
+    const int64_t want = std::min(std::min<int64_t>(4096 / waves, T / 64), int64_t(kMaxSegments));
+    if (waves <= kSplitWaves && want > 1) {
+        p.steps = ceil_div(ceil_div(T, want), 16) * 16;      // whole blocks, in either direction
+        p.segments = ceil_div(T, p.steps);
+    }
     return p;
 }
 
 inline int64_t scan_saved(const snn_scan_cfg* c, int64_t T, int64_t B, int64_t F) {
-    const int64_t states = ceil_div(c->states, kScanStates) * kScanStates;
-    return (ceil_div(T, scan_plan(c, T, B, F).keep) - 1) * B * F * states * 4;
+    return (ceil_div(T, scan_plan(c, T, B, F).keep) - 1) * B * F * scan_held_states(c->states) * 4;
 }
-inline int64_t scan_forward_workspace(const snn_scan_cfg* c, int64_t T, int64_t B, int64_t F) { return 0; }
+// The segments' states and their sums of d.
+inline int64_t scan_part_h(const snn_scan_cfg* c, const ScanPlan& p, int64_t B, int64_t F) {
+    return p.segments > 1 ? p.segments * B * F * scan_held_states(c->states) * 4 : 0;
+}
+inline int64_t scan_part_d(const ScanPlan& p, int64_t B, int64_t F) { return p.segments > 1 ? p.segments * B * F * 4 : 0; }
+inline int64_t scan_forward_workspace(const snn_scan_cfg* c, int64_t T, int64_t B, int64_t F) {
+    const ScanPlan p = scan_plan(c, T, B, F);
+    return piece(scan_part_h(c, p, B, F)) + piece(scan_part_d(p, B, F));
+}
 constexpr int64_t scan_partial_values(int64_t F, int S) { return F * (S + 2); }
 // dL/dB and dL/dC of every tile, as the waves hold them.
 inline int64_t scan_partial_bc(const snn_scan_cfg* c, const ScanPlan& p, int64_t T, int64_t B) {
     return p.tiles * T * B * c->groups * p.waves * 2 * kScanStates * 4;
 }
 inline int64_t scan_backward_workspace(const snn_scan_cfg* c, int64_t T, int64_t B, int64_t F) {
-    return piece(scan_partial_bc(c, scan_plan(c, T, B, F), T, B)) + piece(B * scan_partial_values(F, c->states) * 4);
+    const ScanPlan p = scan_plan(c, T, B, F);
+    return piece(scan_part_h(c, p, B, F)) + piece(scan_part_d(p, B, F)) + piece(scan_partial_bc(c, p, T, B)) +
+           piece(p.segments * B * scan_partial_values(F, c->states) * 4);
 }
 
 struct ScanArgs {
@@ -196,9 +218,12 @@ struct ScanArgs {
     const float* gh_out;
     float *gA, *gD, *gdt_bias, *gh_in;
     float* part_bc;  // backward: [tiles][T][B][G][waves][B, C][4]
-    float* part_f;   // backward: [B] x (A [F][S], D [F], dt_bias [F])
+    float* part_f;   // backward: [segments][B] x (A [F][S], D [F], dt_bias [F])
+    float* part_h;   // several segments: [segments][B][states][F] and [segments][B][F]
+    float* part_d;
     ScanPlan plan;
 };
+snn_status scan_split_entry(int io, bool down, const ScanArgs& a, hipStream_t s);
 snn_status scan_forward_entry(int io, const ScanArgs& a, hipStream_t s);
 snn_status scan_backward_entry(int io, const ScanArgs& a, hipStream_t s);
 

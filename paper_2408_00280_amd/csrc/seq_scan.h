@@ -16,7 +16,7 @@ struct ScanPlace {
     int t0, t1, len;     // the segment, and the steps of the sequence
 };
 
-__device__ __forceinline__ ScanPlace scan_place(const ScanArgs& a) {
+__device__ __forceinline__ ScanPlace scan_place(const ScanArgs& a, int first_segment = 0) {
     ScanPlace p;
     p.lane = threadIdx.x & (kWave - 1);
     p.wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
@@ -30,7 +30,7 @@ __device__ __forceinline__ ScanPlace scan_place(const ScanArgs& a) {
     p.f = p.g * per + (p.active ? j : per - 1);
     p.first = p.wave * kSL;
     p.states = min(kSL, a.S - p.first);
-    p.t0 = int(blockIdx.y * a.plan.steps);
+    p.t0 = int((blockIdx.y + first_segment) * a.plan.steps);
     p.t1 = int(min(a.T, p.t0 + a.plan.steps));
     p.len = __builtin_amdgcn_readfirstlane(steps_of(a.lengths, p.b, a.T));
     return p;
@@ -60,7 +60,7 @@ struct StateColumn {
     float* p;
     int64_t piece, F;
     __device__ StateColumn(const ScanArgs& a, const ScanPlace& s, float* base) : F(a.F) {
-        const int64_t waves = (a.S + kSL - 1) / kSL;
+        const int64_t waves = scan_held_states(a.S) / kSL;
         p = base + (s.b * waves + s.wave) * kSL * F + s.f;
         piece = a.B * waves * kSL * F;
     }

@@ -59,7 +59,8 @@ __global__ __launch_bounds__(NS * kWave, NS > 8 ? 4 : 2) void scan_backward_kern
     const ScanPlace p = scan_place(a);
     float rate[kSL], e[kSL], gA[kSL], gD = 0.0f, gbias = 0.0f;
     load_rates(a, p, rate);
-    load_state(a, p, a.gh_out, e);
+    if (a.plan.segments == 1) load_state(a, p, a.gh_out, e);
+    else if (p.states > 0) StateColumn(a, p, a.part_h).load(blockIdx.y, e);
 #pragma unroll
     for (int i = 0; i < kSL; ++i) gA[i] = 0.0f;
     const float skip = a.D != nullptr ? a.D[p.f] : 0.0f, bias = a.dt_bias != nullptr ? a.dt_bias[p.f] : 0.0f;
@@ -245,7 +246,7 @@ __global__ __launch_bounds__(NS * kWave, NS > 8 ? 4 : 2) void scan_backward_kern
         buf ^= 1;
     }
     if (a.gh_in != nullptr && p.t0 == 0) store_state(a, p, a.gh_in, e);
-    float* pf = a.part_f + p.b * scan_partial_values(a.F, a.S);
+    float* pf = a.part_f + (blockIdx.y * a.B + p.b) * scan_partial_values(a.F, a.S);
 #pragma unroll
     for (int i = 0; i < kSL; ++i)
         if (p.active && i < p.states) pf[p.f * a.S + p.first + i] = gA[i];

@@ -22,7 +22,8 @@ __global__ __launch_bounds__(NS * kWave) void scan_forward_kernel(ScanArgs a) {
     const ScanPlace p = scan_place(a);
     float rate[kSL], h[kSL];
     load_rates(a, p, rate);
-    load_state(a, p, a.h_in, h);
+    if (a.plan.segments == 1) load_state(a, p, a.h_in, h);
+    else if (p.states > 0) StateColumn(a, p, a.part_h).load(blockIdx.y, h);
     const float skip = a.D != nullptr ? a.D[p.f] : 0.0f, bias = a.dt_bias != nullptr ? a.dt_bias[p.f] : 0.0f;
     const Columns<IO> cx(a.x, p), cdt(a.dt, p), cy(a.y, p);
     BCColumns<IO, NS, K> cbc(a, p, p.t0);

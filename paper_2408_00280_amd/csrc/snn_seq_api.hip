@@ -204,6 +204,12 @@ snn_status snn_scan_forward(const snn_scan_cfg* cfg, int64_t T, int64_t B, int64
     a.y = rows(y);
     a.h_out = h_out;
     a.saved = static_cast<float*>(saved);
+    if (a.plan.segments > 1) {
+        int64_t at = 0;
+        a.part_h = carve<float>(workspace, at, scan_part_h(cfg, a.plan, B, F));
+        a.part_d = carve<float>(workspace, at, scan_part_d(a.plan, B, F));
+        if ((st = scan_split_entry(cfg->io, false, a, stream_of(stream))) != SNN_OK) return st;
+    }
     return scan_forward_entry(cfg->io, a, stream_of(stream));
 }
 
@@ -237,8 +243,11 @@ snn_status snn_scan_backward(const snn_scan_cfg* cfg, int64_t T, int64_t B, int6
     a.gdt_bias = grad_dt_bias;
     a.gh_in = grad_h_in;
     int64_t at = 0;
+    a.part_h = carve<float>(workspace, at, scan_part_h(cfg, a.plan, B, F));
+    a.part_d = carve<float>(workspace, at, scan_part_d(a.plan, B, F));
     a.part_bc = carve<float>(workspace, at, scan_partial_bc(cfg, a.plan, T, B));
-    a.part_f = carve<float>(workspace, at, B * scan_partial_values(F, cfg->states) * 4);
+    a.part_f = carve<float>(workspace, at, a.plan.segments * B * scan_partial_values(F, cfg->states) * 4);
+    if (a.plan.segments > 1 && (st = scan_split_entry(io, true, a, stream_of(stream))) != SNN_OK) return st;
     return scan_backward_entry(io, a, stream_of(stream));
 }
 

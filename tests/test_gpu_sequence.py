@@ -153,6 +153,9 @@ SCAN = [
     (20, 1, 72, 64, 2, True, "D bias h", None, "slice"),
     (130, 1, 64, 16, 1, True, "D bias h", None, None),
     (300, 1, 20, 8, 2, True, "D bias", None, None),
+    (270, 4, 70, 16, 1, True, "D bias h", "ragged", "batch"),     # several segments of the time axis
+    (333, 3, 65, 33, 1, True, "bias h", "ragged", None),
+    (150, 2, 130, 2, 2, False, "h", "ragged", "slice"),
 ]
 
 
