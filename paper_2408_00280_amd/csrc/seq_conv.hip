@@ -1,11 +1,11 @@
 // Short causal convolution along time, forward and backward.
 //
-// A lane owns V neighbouring features (16 bytes of a row) of one sequence and walks a chunk
+// A lane owns V neighbouring features (8 or 16 bytes of a row) of one sequence and walks a chunk
 // of its steps with the last W-1 inputs in registers, so each input is read once, but for
 // W-1 rows at a chunk's start.  The backward walks W-1 steps past its chunk: dL/dx[s] needs
 // dL/du of steps s to s+W-1, whose activation it recomputes from x.  Sums over steps for the
 // filter's gradient stay in registers per chunk and are then added up by a second kernel.
-// Bound by memory.
+// The next rows are loaded while these are computed.  Bound by memory.
 #include "seq_device.h"
 
 namespace snnlif {
@@ -63,9 +63,13 @@ __device__ void conv_state(const ConvArgs& a, int64_t len, int64_t b, int64_t f)
         IoVec<IO, V>::store(a.state_out, (i * a.B + b) * a.F + f, v[i]);
 }
 
+__host__ __device__ bool conv_state_later(const ConvArgs& a) {
+    return a.plan.chunks > 1 && a.state_out == a.state_in;
+}
+
 template <int IO, int W, int ACT, int V>
 __device__ void conv_forward_walk(const ConvArgs& a, const ConvLane& l) {
-    constexpr int U = 8;     // rows in flight
+    constexpr int U = conv_rows(false);     // rows in flight
     float w[V][W], bias[V], hist[W][V];
     load_filter<W, V>(a, l.f, w, bias);
     const int64_t len = steps_of(a.lengths, l.b, a.T), t0 = l.c * a.plan.steps;
@@ -74,11 +78,17 @@ __device__ void conv_forward_walk(const ConvArgs& a, const ConvLane& l) {
 #pragma unroll
         for (int i = 0; i < W - 1; ++i) conv_input<IO, W, V>(a, t0 - (W - 1) + i, l.b, l.f, hist[i]);
     }
-    for (int64_t t = t0; t < stop; t += U) {
-        typename IoVec<IO, V>::raw raw[U];
+    typename IoVec<IO, V>::raw raw[U], ahead[U];
+    const auto fetch = [&](int64_t t) {
 #pragma unroll
         for (int k = 0; k < U; ++k)
-            if (t + k < stop) raw[k] = IoVec<IO, V>::load(at<IO>(a.x, t + k, l.b, l.f), 0);
+            if (t + k < stop) ahead[k] = IoVec<IO, V>::load(at<IO>(a.x, t + k, l.b, l.f), 0);
+    };
+    fetch(t0);
+    for (int64_t t = t0; t < stop; t += U) {
+#pragma unroll
+        for (int k = 0; k < U; ++k) raw[k] = ahead[k];
+        fetch(t + U);
 #pragma unroll
         for (int k = 0; k < U; ++k) {
             if (t + k < stop) {
@@ -99,13 +109,15 @@ __device__ void conv_forward_walk(const ConvArgs& a, const ConvLane& l) {
     }
     float zero[V] = {};
     for (int64_t t = max(t0, stop); t < end; ++t) IoVec<IO, V>::store(at_out<IO>(a.y, t, l.b, l.f), 0, zero);
-    // one chunk: this lane alone reads and writes its features' state
-    if (a.plan.chunks == 1 && a.state_out != nullptr) conv_state<IO, W, V>(a, len, l.b, l.f);
+    // The chunk with the sequence's last step leaves the state.  In place that is safe for one
+    // chunk only, whose lane alone reads and writes its features' state.
+    const bool own = t0 < max(len, int64_t(1)) && len <= end;
+    if (a.state_out != nullptr && own && !conv_state_later(a)) conv_state<IO, W, V>(a, len, l.b, l.f);
 }
 
 template <int IO, int W, int ACT>
 __global__ __launch_bounds__(kBlock) void conv_forward_kernel(ConvArgs a) {
-    constexpr int V = IO == SNN_IO_F32 ? 4 : 8;
+    constexpr int V = conv_vec(IO, false);
     bool any;
     const ConvLane l = conv_lane<V>(a, any);
     if (!any) return;
@@ -113,10 +125,10 @@ __global__ __launch_bounds__(kBlock) void conv_forward_kernel(ConvArgs a) {
     else conv_forward_walk<IO, W, ACT, 1>(a, l);
 }
 
-// The state behind several chunks, once all of them have read the one before.
+// The state in place behind several chunks, once all of them have read the one before.
 template <int IO, int W>
 __global__ __launch_bounds__(kBlock) void conv_state_kernel(ConvArgs a) {
-    constexpr int V = IO == SNN_IO_F32 ? 4 : 8;
+    constexpr int V = conv_vec(IO, false);
     bool any;
     const ConvLane l = conv_lane<V>(a, any);
     if (!any || l.c != 0) return;
@@ -127,7 +139,7 @@ __global__ __launch_bounds__(kBlock) void conv_state_kernel(ConvArgs a) {
 
 template <int IO, int W, int ACT, int V>
 __device__ void conv_backward_walk(const ConvArgs& a, const ConvLane& l) {
-    constexpr int U = 4;
+    constexpr int U = conv_rows(true);
     float w[V][W], bias[V], hist[W][V], gu[W][V], gw[V][W], gb[V];
     load_filter<W, V>(a, l.f, w, bias);
     const int64_t len = steps_of(a.lengths, l.b, a.T), t0 = l.c * a.plan.steps;
@@ -170,15 +182,24 @@ __device__ void conv_backward_walk(const ConvArgs& a, const ConvLane& l) {
         const int64_t past = min(len, end + (W - 1));   // steps whose dL/du this chunk needs
 #pragma unroll
         for (int i = 0; i < W - 1; ++i) conv_input<IO, W, V>(a, t0 - (W - 1) + i, l.b, l.f, hist[i]);
-        for (int64_t t = t0; t < past; t += U) {
-            typename IoVec<IO, V>::raw xr[U], gr[U];
+        typename IoVec<IO, V>::raw xr[U], gr[U], xa[U], ga[U];
+        const auto fetch = [&](int64_t t) {
 #pragma unroll
             for (int k = 0; k < U; ++k) {
                 if (t + k < past) {
-                    xr[k] = IoVec<IO, V>::load(at<IO>(a.x, t + k, l.b, l.f), 0);
-                    gr[k] = IoVec<IO, V>::load(at<IO>(a.gy, t + k, l.b, l.f), 0);
+                    xa[k] = IoVec<IO, V>::load(at<IO>(a.x, t + k, l.b, l.f), 0);
+                    ga[k] = IoVec<IO, V>::load(at<IO>(a.gy, t + k, l.b, l.f), 0);
                 }
             }
+        };
+        fetch(t0);
+        for (int64_t t = t0; t < past; t += U) {
+#pragma unroll
+            for (int k = 0; k < U; ++k) {
+                xr[k] = xa[k];
+                gr[k] = ga[k];
+            }
+            fetch(t + U);
 #pragma unroll
             for (int k = 0; k < U; ++k) {
                 if (t + k < past) {
@@ -225,7 +246,7 @@ __device__ void conv_backward_walk(const ConvArgs& a, const ConvLane& l) {
 
 template <int IO, int W, int ACT>
 __global__ __launch_bounds__(kBlock) void conv_backward_kernel(ConvArgs a) {
-    constexpr int V = IO == SNN_IO_F32 ? 4 : 8;
+    constexpr int V = conv_vec(IO, true);
     bool any;
     const ConvLane l = conv_lane<V>(a, any);
     if (!any) return;
@@ -238,7 +259,7 @@ snn_status conv_forward_w(int act, const ConvArgs& a, hipStream_t s) {
     const dim3 grid = grid_for(a.plan.lanes * a.B * a.plan.chunks);
     const snn_status st = act == SNN_ACT_SILU ? launch(conv_forward_kernel<IO, W, SNN_ACT_SILU>, grid, s, a)
                                               : launch(conv_forward_kernel<IO, W, SNN_ACT_NONE>, grid, s, a);
-    if (st != SNN_OK || a.plan.chunks == 1 || a.state_out == nullptr || W == 1) return st;
+    if (st != SNN_OK || a.state_out == nullptr || W == 1 || !conv_state_later(a)) return st;
     return launch(conv_state_kernel<IO, W>, grid_for(a.plan.lanes * a.B), s, a);
 }
 

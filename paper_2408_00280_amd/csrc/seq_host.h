@@ -94,22 +94,25 @@ inline snn_status check_conv_cfg(const snn_conv_cfg* c) {
     return c->act == SNN_ACT_NONE || c->act == SNN_ACT_SILU ? SNN_OK : SNN_E_PARAM;
 }
 
-// Lanes own 16 bytes of features (the few left over one each) and walk `steps` steps of one
-// sequence; there are `chunks` such pieces of the time axis.  Eight waves per CU keep enough
-// loads in flight; shorter walks than 16 steps read too much of their neighbours' inputs.
+// Lanes own V neighbouring features (the few left over one each) and walk `steps` steps of one
+// sequence, U rows at a time; there are `chunks` such pieces of the time axis.  2^18 lanes in
+// the forward and 2^17 in the backward, which holds more of a chunk and leaves a partial sum
+// for each, did best of 2^16 to 2^19 (x[2048][8][4096] bf16: 62.5 of 62-74 us, 97 of 97-122 us).
+// A chunk has U steps at least, as W-1 of them are read twice.
 struct ConvPlan {
     int64_t lanes;   // per sequence and chunk
     int64_t steps, chunks;
 };
 
-inline int conv_vec(int io) { return io == SNN_IO_F32 ? 4 : 8; }
+constexpr int conv_vec(int io, bool backward) { return io == SNN_IO_F32 || backward ? 4 : 8; }
+constexpr int conv_rows(bool backward) { return backward ? 4 : 8; }
 
-inline ConvPlan conv_plan(const snn_conv_cfg* c, int64_t T, int64_t B, int64_t F) {
-    const int v = conv_vec(c->io);
+inline ConvPlan conv_plan(const snn_conv_cfg* c, int64_t T, int64_t B, int64_t F, bool backward) {
+    const int v = conv_vec(c->io, backward);
     ConvPlan p;
     p.lanes = F / v + F % v;
-    const int64_t want = ceil_div(int64_t(1) << 17, p.lanes * B);
-    p.steps = std::max<int64_t>(16, ceil_div(T, want));
+    const int64_t want = ceil_div(int64_t(1) << (backward ? 17 : 18), p.lanes * B);
+    p.steps = std::max<int64_t>(8, ceil_div(T, want));
     p.chunks = ceil_div(T, p.steps);
     return p;
 }
@@ -117,7 +120,7 @@ inline ConvPlan conv_plan(const snn_conv_cfg* c, int64_t T, int64_t B, int64_t F
 inline int64_t conv_partial(const snn_conv_cfg* c, int64_t F) { return F * (c->width + 1); }
 
 inline int64_t conv_workspace(const snn_conv_cfg* c, int64_t T, int64_t B, int64_t F) {
-    return piece(conv_plan(c, T, B, F).chunks * B * conv_partial(c, F) * 4);
+    return piece(conv_plan(c, T, B, F, true).chunks * B * conv_partial(c, F) * 4);
 }
 
 struct ConvArgs {
@@ -144,7 +147,7 @@ inline snn_status check_scan_cfg(const snn_scan_cfg* c) {
 }
 
 constexpr int kScanStates = 4;   // states per lane
-constexpr int kScanBlock = 8;    // steps that the waves share out at a time
+constexpr int kScanBlock = 8;    // steps that the waves of the local pass share out at a time
 constexpr int64_t kSplitWaves = 1024, kMaxSegments = 1024;
 
 // A workgroup owns 64 features of one group and one sequence, a feature per lane; each of its

@@ -13,9 +13,9 @@
 namespace snnlif {
 namespace {
 
-template <int IO, int NS>
+template <int IO, int NS, int K>
 __global__ __launch_bounds__(NS * kWave) void scan_forward_kernel(ScanArgs a) {
-    constexpr int K = kScanBlock, R = K > NS ? K / NS : 1, U = 2;   // U: steps read from LDS ahead
+    constexpr int R = K > NS ? K / NS : 1, U = 2;   // U: steps read from LDS ahead
     __shared__ float2 sd[3][K][kWave];           // (d, d x): of this block, the next and the one being staged
     __shared__ float sy[2][NS][K][kWave];
     __shared__ __align__(16) StagedBC<NS, K> sbc[3];
@@ -133,15 +133,131 @@ __global__ __launch_bounds__(NS * kWave) void scan_forward_kernel(ScanArgs a) {
     if (a.h_out != nullptr && p.t1 == a.T) store_state(a, p, a.h_out, h);
 }
 
+// One step: a feature's states lie over Q neighbouring lanes, 4 each, so that the state is read
+// and written once, 16 bytes per lane and contiguously; y is their sum over the Q lanes.  A
+// lane takes the same states of N sequences, whose loads are all in flight at once.  Bound by
+// memory: the states are all but a few percent of what moves.
+template <int IO, int Q, int N>
+__global__ __launch_bounds__(kBlock) void scan_token_kernel(ScanArgs a) {
+    const int64_t i = int64_t(blockIdx.x) * kBlock + threadIdx.x;
+    const unsigned F = unsigned(a.F), B = unsigned(a.B), n = (B + N - 1) / N * F, bf = min(unsigned(i / Q), n - 1);
+    const bool active = i / Q < n;               // lanes behind the last feature compute it again
+    const unsigned b0 = bf / F * N, f = bf % F, g = f / (F / unsigned(a.G));
+    const int q = int(i) & (Q - 1), s0 = q * kSL, states = max(0, min(kSL, a.S - s0));
+    const auto load4 = [&](const float* p, float (&v)[kSL]) {
+        if (states == kSL) {
+            const f32x4_t r = ld_nt<f32x4_t>(p);
+#pragma unroll
+            for (int j = 0; j < kSL; ++j) v[j] = r[j];
+        } else {
+#pragma unroll
+            for (int j = 0; j < kSL; ++j) v[j] = j < states ? p[j] : 0.0f;
+        }
+    };
+    const auto load_io = [&](const Rows& r, unsigned b, float (&v)[kSL]) {
+        if (states == kSL) {
+            load_vec<IO, kSL>(at<IO>(r, 0, b, int64_t(g) * a.S + s0), v);
+        } else {
+#pragma unroll
+            for (int j = 0; j < kSL; ++j)
+                v[j] = j < states ? load1<IO>(at<IO>(r, 0, b, int64_t(g) * a.S + s0 + j)) : 0.0f;
+        }
+    };
+    float h[N][kSL], bv[N][kSL], cv[N][kSL], x[N], v[N], rate[kSL];
+    bool on[N];
+#pragma unroll
+    for (int k = 0; k < N; ++k) {
+        const unsigned b = b0 + k;
+        on[k] = b < B && steps_of(a.lengths, b, a.T) > 0;
+        if (b < B && a.h_in != nullptr) {
+            load4(a.h_in + (int64_t(b) * F + f) * a.S + s0, h[k]);
+        } else {
+#pragma unroll
+            for (int j = 0; j < kSL; ++j) h[k][j] = 0.0f;
+        }
+        if (on[k]) {
+            load_io(a.Bm, b, bv[k]);
+            load_io(a.Cm, b, cv[k]);
+            x[k] = load1<IO>(at<IO>(a.x, 0, b, f));
+            v[k] = load1<IO>(at<IO>(a.dt, 0, b, f));
+        }
+    }
+    load4(a.A + int64_t(f) * a.S + s0, rate);
+    const float bias = a.dt_bias != nullptr ? a.dt_bias[f] : 0.0f, skip = a.D != nullptr ? a.D[f] : 0.0f;
+#pragma unroll
+    for (int k = 0; k < N; ++k) {
+        const unsigned b = b0 + k;
+        float y = 0.0f;
+        if (on[k]) {
+            const float w = v[k] + bias, d = a.softplus ? softplus(w) : w;
+#pragma unroll
+            for (int j = 0; j < kSL; ++j) {
+                h[k][j] = fmaf(__builtin_amdgcn_exp2f(d * (rate[j] * kLog2e)), h[k][j], (d * x[k]) * bv[k][j]);
+                y = fmaf(cv[k][j], h[k][j], y);
+            }
+            y = q == 0 ? fmaf(skip, x[k], y) : y;
+        }
+        if (Q > 1) y += dpp<kDppXor1>(y);
+        if (Q > 2) y += dpp<kDppXor2>(y);
+        if (Q > 4) y += dpp<kDppHalfMirror>(y);
+        if (Q > 8) y += dpp<kDppRor8>(y);
+        if (!active || b >= B) continue;
+        if (q == 0) store1<IO>(at_out<IO>(a.y, 0, b, f), y);
+        if (a.h_out != nullptr) {
+            float* to = a.h_out + (int64_t(b) * F + f) * a.S + s0;
+            if (states == kSL) {
+                const f32x4_t r = {h[k][0], h[k][1], h[k][2], h[k][3]};
+                st_nt(to, r);
+            } else {
+#pragma unroll
+                for (int j = 0; j < kSL - 1; ++j)
+                    if (j < states) to[j] = h[k][j];
+            }
+        }
+    }
+}
+
+template <int IO, int Q>
+snn_status token_lanes(const ScanArgs& a, hipStream_t s) {
+    // several sequences per lane where that leaves 16 waves per CU
+    if (a.B * a.F * Q >= int64_t(4) * 256 * 16 * kWave)
+        return launch(scan_token_kernel<IO, Q, 4>, grid_for(ceil_div(a.B, 4) * a.F * Q), s, a);
+    return launch(scan_token_kernel<IO, Q, 1>, grid_for(a.B * a.F * Q), s, a);
+}
+
+template <int IO>
+snn_status token_states(const ScanArgs& a, hipStream_t s) {
+    switch (a.plan.waves) {                      // the lanes per feature
+        case 1: return token_lanes<IO, 1>(a, s);
+        case 2: return token_lanes<IO, 2>(a, s);
+        case 4: return token_lanes<IO, 4>(a, s);
+        case 8: return token_lanes<IO, 8>(a, s);
+        default: return token_lanes<IO, 16>(a, s);
+    }
+}
+
+template <int IO, int NS>
+snn_status forward_waves(const ScanArgs& a, hipStream_t s) {
+    const dim3 grid(unsigned(a.plan.tiles * a.G * a.B), unsigned(a.plan.segments));
+    // Up to two workgroups of four waves per CU have the LDS for blocks of 16 steps, whose
+    // barriers are half as many (x[1024][8][4096]: 218 us to 244 with blocks of 8); more of
+    // them hide the barriers themselves and need blocks of 8 to fit (x[4096][1][4096] in 16
+    // segments: 88 us to 103 with blocks of 16).
+    if constexpr (NS == 4) {
+        if (int64_t(grid.x) * grid.y <= 2 * 256) return launch_blk(scan_forward_kernel<IO, NS, 16>, grid, NS * kWave, s, a);
+    }
+    return launch_blk(scan_forward_kernel<IO, NS, 8>, grid, NS * kWave, s, a);
+}
+
 template <int IO>
 snn_status forward_io(const ScanArgs& a, hipStream_t s) {
-    const dim3 grid(unsigned(a.plan.tiles * a.G * a.B), unsigned(a.plan.segments));
+    if (a.T == 1) return token_states<IO>(a, s);
     switch (a.plan.waves) {
-        case 1: return launch_blk(scan_forward_kernel<IO, 1>, grid, 1 * kWave, s, a);
-        case 2: return launch_blk(scan_forward_kernel<IO, 2>, grid, 2 * kWave, s, a);
-        case 4: return launch_blk(scan_forward_kernel<IO, 4>, grid, 4 * kWave, s, a);
-        case 8: return launch_blk(scan_forward_kernel<IO, 8>, grid, 8 * kWave, s, a);
-        default: return launch_blk(scan_forward_kernel<IO, 16>, grid, 16 * kWave, s, a);
+        case 1: return forward_waves<IO, 1>(a, s);
+        case 2: return forward_waves<IO, 2>(a, s);
+        case 4: return forward_waves<IO, 4>(a, s);
+        case 8: return forward_waves<IO, 8>(a, s);
+        default: return forward_waves<IO, 16>(a, s);
     }
 }
 

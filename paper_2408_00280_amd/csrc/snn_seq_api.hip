@@ -24,8 +24,11 @@ snn_status check_conv(const snn_conv_cfg* c, int64_t T, int64_t B, int64_t F) {
     if (st != SNN_OK) return st;
     if (check_seq_shape(T, B, F) != SNN_OK) return SNN_E_SHAPE;
     if (empty(T, B, F)) return SNN_OK;
-    const ConvPlan p = conv_plan(c, T, B, F);
-    return ceil_div(p.lanes * B * p.chunks, kBlock) <= kMaxBlocks ? SNN_OK : SNN_E_SHAPE;
+    for (bool backward : {false, true}) {
+        const ConvPlan p = conv_plan(c, T, B, F, backward);
+        if (ceil_div(p.lanes * B * p.chunks, kBlock) > kMaxBlocks) return SNN_E_SHAPE;
+    }
+    return SNN_OK;
 }
 
 snn_status check_scan(const snn_scan_cfg* c, int64_t T, int64_t B, int64_t F) {
@@ -35,7 +38,7 @@ snn_status check_scan(const snn_scan_cfg* c, int64_t T, int64_t B, int64_t F) {
     if (F % c->groups != 0) return SNN_E_SHAPE;
     if (empty(T, B, F)) return SNN_OK;
     const ScanPlan p = scan_plan(c, T, B, F);
-    if (p.tiles * c->groups > kMaxBlocks / B) return SNN_E_SHAPE;
+    if (p.tiles * c->groups > kMaxBlocks / B || F > kMaxN / B) return SNN_E_SHAPE;
     return T * B * c->groups <= kMaxBlocks && F * c->states <= kMaxSpan / B ? SNN_OK : SNN_E_SHAPE;
 }
 
@@ -126,7 +129,7 @@ snn_status snn_conv_forward(const snn_conv_cfg* cfg, int64_t T, int64_t B, int64
     a.state_in = state_in;
     a.lengths = lengths;
     a.state_out = state_out;
-    a.plan = conv_plan(cfg, T, B, F);
+    a.plan = conv_plan(cfg, T, B, F, false);
     return conv_forward_entry(cfg, a, stream_of(stream));
 }
 
@@ -165,7 +168,7 @@ snn_status snn_conv_backward(const snn_conv_cfg* cfg, int64_t T, int64_t B, int6
     a.gstate_out = grad_state_out;
     a.gstate_in = grad_state_in;
     a.part = static_cast<float*>(workspace);
-    a.plan = conv_plan(cfg, T, B, F);
+    a.plan = conv_plan(cfg, T, B, F, true);
     st = conv_backward_entry(cfg, a, stream_of(stream));
     if (st != SNN_OK) return st;
     const ReduceOut out = {{grad_weight, grad_bias, nullptr}, {F * cfg->width, F, 0}};

@@ -156,6 +156,7 @@ SCAN = [
     (270, 4, 70, 16, 1, True, "D bias h", "ragged", "batch"),     # several segments of the time axis
     (333, 3, 65, 33, 1, True, "bias h", "ragged", None),
     (150, 2, 130, 2, 2, False, "h", "ragged", "slice"),
+    (1, 33, 2100, 62, 3, True, "D bias h", "ragged", "slice"),    # several sequences per lane
 ]
 
 
