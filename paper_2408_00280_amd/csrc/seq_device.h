@@ -54,11 +54,19 @@ __device__ __forceinline__ float silu_slope(float u, float s) { return s * fmaf(
 
 // ln(1 + e^v) = max(v, 0) + ln(1 + e), e = e^-|v| <= 1.  ln(1 + e) loses e's low bits in the
 // sum w = 1 + e; ln(w) e / (w - 1) puts them back (Kahan), as w - 1 is exact.
-__device__ __forceinline__ float softplus(float v) {
-    const float e = __builtin_amdgcn_exp2f(-kLog2e * fabsf(v));
+__device__ __forceinline__ float softplus_of(float v, float e) {
     const float w = 1.0f + e, d = w - 1.0f;
     const float l = (kLn2 * __builtin_amdgcn_logf(w)) * (e * __builtin_amdgcn_rcpf(d));
     return fmaxf(v, 0.0f) + (d == 0.0f ? e : l);
+}
+__device__ __forceinline__ float softplus(float v) {
+    return softplus_of(v, __builtin_amdgcn_exp2f(-kLog2e * fabsf(v)));
+}
+// With its slope, the sigmoid of v.
+__device__ __forceinline__ float softplus(float v, float& slope) {
+    const float e = __builtin_amdgcn_exp2f(-kLog2e * fabsf(v)), r = __builtin_amdgcn_rcpf(1.0f + e);
+    slope = v < 0.0f ? e * r : r;
+    return softplus_of(v, e);
 }
 
 template <int CTRL>

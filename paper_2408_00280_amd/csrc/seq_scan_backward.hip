@@ -5,9 +5,9 @@
 //   dL/d(d) = sum_n dL/dh (A a h[t-1] + B x),  dL/dA += dL/dh d a h[t-1],
 //   dL/dx = sum_n dL/dh B d + D dL/dy,  dL/ddt = dL/d(d) sigmoid(dt + dt_bias).
 // Blocks of K steps go in reverse: from the state that the forward kept at the block's start
-// the decays a and the products a h[t-1] of its steps are formed again in registers, then the
-// recurrence runs down.  Lanes, waves and scalars are as in the forward, and as there the next
-// block is staged and the one after is loaded while a block runs.  The sums of dL/dB and dL/dC
+// the decays and states of its steps are formed again in registers, then the recurrence runs
+// down, dL/dh a h[t-1] as e[t-1] h[t-1].  Lanes, waves and scalars are as in the forward, and as there the next
+// block is loaded while a block runs.  The sums of dL/dB and dL/dC
 // over the 64 features of a wave halve the number of values at each of the first three steps
 // (8 values and 64 lanes to 1 value in 8 groups of lanes): 17 instructions for 4 states.  Sums
 // over tiles, sequences and steps go through partial results that further kernels add up in a
@@ -53,7 +53,7 @@ struct BackwardLds {
 
 template <int IO, int NS>
 __global__ __launch_bounds__(NS * kWave, NS > 8 ? 4 : 2) void scan_backward_kernel(ScanArgs a) {
-    constexpr int K = scan_keep(NS), R = K > NS ? K / NS : 1, U = 1;
+    constexpr int K = scan_keep(NS), R = K > NS ? K / NS : 1;
     extern __shared__ __align__(16) char lds[];
     auto& m = *reinterpret_cast<BackwardLds<NS>*>(lds);
     const ScanPlace p = scan_place(a);
@@ -71,7 +71,8 @@ __global__ __launch_bounds__(NS * kWave, NS > 8 ? 4 : 2) void scan_backward_kern
     struct Raw {
         typename IoVec<IO, 1>::raw x, dt, gy;
     };
-    Raw raw[R], own[R];          // of the next block; of this block, for its end
+    Raw raw[R];                  // of the next block
+    float own[R][2];             // x and the softplus' slope of this block, for its end
     const auto fetch_rows = [&](int t0) {
 #pragma unroll
         for (int r = 0; r < R; ++r) {
@@ -79,14 +80,16 @@ __global__ __launch_bounds__(NS * kWave, NS > 8 ? 4 : 2) void scan_backward_kern
             if (k < K && t0 >= p.t0 && t0 + k < p.len) raw[r] = {cx.load(t0 + k), cdt.load(t0 + k), cgy.load(t0 + k)};
         }
     };
-    const auto stage_rows = [&](int t0, int to) {
+    const auto stage_rows = [&](int t0, int to, float (&mine)[R][2]) {
 #pragma unroll
         for (int r = 0; r < R; ++r) {
             const int k = p.wave + r * NS;
             Step d = {0.0f, 0.0f, 0.0f};
             if (k < K && t0 >= p.t0 && t0 + k < p.len) {
                 const float v = IoVec<IO, 1>::get(raw[r].dt, 0) + bias, x = IoVec<IO, 1>::get(raw[r].x, 0);
-                d.d = a.softplus ? softplus(v) : v;
+                mine[r][0] = x;
+                mine[r][1] = 1.0f;
+                d.d = a.softplus ? softplus(v, mine[r][1]) : v;
                 if (p.active) {                  // lanes behind the group add nothing
                     d.dx = d.d * x;
                     d.gy = IoVec<IO, 1>::get(raw[r].gy, 0);
@@ -111,20 +114,18 @@ __global__ __launch_bounds__(NS * kWave, NS > 8 ? 4 : 2) void scan_backward_kern
         cbc.template fetch<-1>(t0, p.t0, p.len);
         fetch_rows(t0);
     };
-    const auto stage = [&](int t0, int to) {
+    const auto stage = [&](int t0, int to, float (&mine)[R][2]) {
         if (t0 >= p.t0) cbc.stage(t0, p.len, m.sbc[to]);
-        stage_rows(t0, to);
+        stage_rows(t0, to, mine);
     };
     fetch(t0);
-    stage(t0, 0);
-#pragma unroll
-    for (int r = 0; r < R; ++r) own[r] = raw[r];
+    stage(t0, 0, own);
     fetch(t0 - K);
     float h[kSL], h_next[kSL];
     struct Ahead {
         Step d;
         f32x4_t b, c;
-    } step[U], ahead[U];
+    } step, ahead;
     const auto read = [&](int block, int k) {
         const f32x4_t* bc = reinterpret_cast<const f32x4_t*>(m.sbc[block].v[k][p.wave]);
         return Ahead{m.sd[block][k][p.lane], bc[0], bc[1]};
@@ -135,74 +136,61 @@ __global__ __launch_bounds__(NS * kWave, NS > 8 ? 4 : 2) void scan_backward_kern
     int buf = 0;
     for (; t0 >= p.t0; t0 -= K) {
         const int below = max(t0 - K, p.t0);
-        Raw staged[R];
-        stage(t0 - K, buf ^ 1);
-#pragma unroll
-        for (int r = 0; r < R; ++r) staged[r] = raw[r];
-        fetch(t0 - 2 * K);
         if (busy) {
+            step = read(buf, 0);
+            float dec[K][kSL], hs[K + 1][kSL];       // decays, and the states before each step
 #pragma unroll
-            for (int i = 0; i < U; ++i) step[i] = read(buf, i);
-            if (below > 0) kept.load(below / K - 1, h_next);
-            else load_state(a, p, a.h_in, h_next);
-            float dec[K][kSL], ah[K][kSL];
+            for (int s = 0; s < kSL; ++s) hs[0][s] = h[s];
 #pragma unroll
-            for (int u = 0; u < K; u += U) {
-                if (u + U < K) {
-#pragma unroll
-                    for (int i = 0; i < U; ++i) ahead[i] = read(buf, u + U + i);
-                }
+            for (int k = 0; k < K; ++k) {
+                if (k + 1 < K) ahead = read(buf, k + 1);
                 __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-                for (int i = 0; i < U; ++i) {
-#pragma unroll
-                    for (int s = 0; s < kSL; ++s) {
-                        dec[u + i][s] = __builtin_amdgcn_exp2f(step[i].d.d * rate[s]);
-                        ah[u + i][s] = dec[u + i][s] * h[s];
-                        h[s] = fmaf(step[i].d.dx, step[i].b[s], ah[u + i][s]);
-                    }
+                for (int s = 0; s < kSL; ++s) {
+                    dec[k][s] = __builtin_amdgcn_exp2f(step.d.d * rate[s]);
+                    hs[k + 1][s] = fmaf(dec[k][s], hs[k][s], step.d.dx * step.b[s]);
                 }
                 __builtin_amdgcn_sched_barrier(0);
-                if (u + U < K) {
-#pragma unroll
-                    for (int i = 0; i < U; ++i) step[i] = ahead[i];
-                }
+                if (k + 1 < K) step = ahead;
             }
+            // the sums over the wave run a step behind, beside the next step's recurrence
+            float v[2 * kSL];
+            const auto sum_up = [&](int k) {
+                m.sgbc[k][p.wave][p.lane >> 3] = reduce8(v, p.lane);   // the same from 8 lanes
+            };
 #pragma unroll
-            for (int u = K - U; u >= 0; u -= U) {
-                if (u > 0) {
-#pragma unroll
-                    for (int i = 0; i < U; ++i) ahead[i] = read(buf, u - U + i);
+            for (int k = K - 1; k >= 0; --k) {
+                if (k > 0) ahead = read(buf, k - 1);
+                if (k == K / 2) {                // half of the block's registers are free by now
+                    if (below > 0) kept.load(below / K - 1, h_next);
+                    else load_state(a, p, a.h_in, h_next);
                 }
                 __builtin_amdgcn_sched_barrier(0);
+                if (k < K - 1) sum_up(k + 1);
+                const Step d = step.d;
+                float gx = 0.0f, gd = 0.0f;
 #pragma unroll
-                for (int i = U - 1; i >= 0; --i) {
-                    const Step d = step[i].d;
-                    float v[8], gx = 0.0f, gd = 0.0f;
-#pragma unroll
-                    for (int s = 0; s < kSL; ++s) {
-                        const float b = step[i].b[s], dh = fmaf(step[i].c[s], d.gy, e[s]);
-                        v[s] = dh * d.dx;
-                        v[kSL + s] = d.gy * fmaf(d.dx, b, ah[u + i][s]);
-                        gx = fmaf(dh, b, gx);
-                        const float q = dh * ah[u + i][s];
-                        gd = fmaf(q, rate[s], gd);
-                        gA[s] = fmaf(q, d.d, gA[s]);
-                        e[s] = dec[u + i][s] * dh;
-                    }
-                    m.sg[p.wave][u + i][p.lane] = {gx, gd};
-                    const float r = reduce8(v, p.lane);
-                    if ((p.lane & 7) == 0) m.sgbc[u + i][p.wave][p.lane >> 3] = r;
+                for (int s = 0; s < kSL; ++s) {
+                    const float b = step.b[s], dh = fmaf(step.c[s], d.gy, e[s]);
+                    v[s] = dh * d.dx;
+                    v[kSL + s] = d.gy * hs[k + 1][s];
+                    gx = fmaf(dh, b, gx);
+                    e[s] = dec[k][s] * dh;
+                    const float q = e[s] * hs[k][s];
+                    gd = fmaf(q, rate[s], gd);
+                    gA[s] = fmaf(q, d.d, gA[s]);
                 }
+                m.sg[p.wave][k][p.lane] = {gx, gd};
                 __builtin_amdgcn_sched_barrier(0);
-                if (u > 0) {
-#pragma unroll
-                    for (int i = 0; i < U; ++i) step[i] = ahead[i];
-                }
+                step = ahead;
             }
+            sum_up(0);
 #pragma unroll
             for (int s = 0; s < kSL; ++s) h[s] = h_next[s];
         }
+        float staged[R][2];
+        stage(t0 - K, buf ^ 1, staged);
+        fetch(t0 - 2 * K);
         lds_barrier();
 #pragma unroll
         for (int r = 0; r < R; ++r) {
@@ -221,9 +209,8 @@ __global__ __launch_bounds__(NS * kWave, NS > 8 ? 4 : 2) void scan_backward_kern
                         da += w < used ? g[w].y : 0.0f;
                     }
                     gx = fmaf(s.d, db, skip * s.gy);
-                    const float x = IoVec<IO, 1>::get(own[r].x, 0);
-                    gdt = fmaf(x, db, da * kLn2);                // rate is A log2 e
-                    if (a.softplus) gdt *= sigmoid(IoVec<IO, 1>::get(own[r].dt, 0) + bias);
+                    const float x = own[r][0];
+                    gdt = fmaf(x, db, da * kLn2) * own[r][1];    // rate is A log2 e
                     gD = fmaf(s.gy, x, gD);
                     gbias += gdt;
                 }
@@ -232,7 +219,8 @@ __global__ __launch_bounds__(NS * kWave, NS > 8 ? 4 : 2) void scan_backward_kern
                     cgdt.store(t0 + k, gdt);
                 }
             }
-            own[r] = staged[r];
+            own[r][0] = staged[r][0];
+            own[r][1] = staged[r][1];
         }
         {
             const int64_t row = int64_t(a.B) * a.G * (NS * 2 * kSL);
