@@ -210,8 +210,20 @@ struct Lane8 {
     // Parameters: `other` where there are none, 0 behind the row's end.
     __device__ void params(const float* p, float other, float (&v)[kNormLane]) const {
 #pragma unroll
-        for (int i = 0; i < kNormLane; ++i)
-            v[i] = i % V < n[i / V] ? (p != nullptr ? p[f[i / V] + i % V] : other) : 0.0f;
+        for (int c = 0; c < N; ++c) {
+            if (p != nullptr && n[c] == V) {
+#pragma unroll
+                for (int j = 0; j < V; j += 4) {
+                    typedef f32x4_t vec __attribute__((aligned(4)));
+                    const f32x4_t w = *reinterpret_cast<const vec*>(p + f[c] + j);
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) v[c * V + j + i] = w[i];
+                }
+            } else {
+#pragma unroll
+                for (int j = 0; j < V; ++j) v[c * V + j] = j < n[c] ? (p != nullptr ? p[f[c] + j] : other) : 0.0f;
+            }
+        }
     }
     __device__ void put(float* p, const float (&v)[kNormLane]) const {
 #pragma unroll

@@ -22,6 +22,9 @@ from . import native
 IO_OF = {torch.float32: native.SNN_IO_F32, torch.bfloat16: native.SNN_IO_BF16}
 ACTS = {None: native.SNN_ACT_NONE, "silu": native.SNN_ACT_SILU}
 
+_conv_cfg, _scan_cfg, _norm_cfg = (functools.lru_cache(maxsize=64)(c) for c in (
+    native.snn_conv_cfg, native.snn_scan_cfg, native.snn_norm_cfg))
+
 
 def _on_stream(fn):
     """fn with its first tensor's device as the current one, on `stream`."""
@@ -47,36 +50,33 @@ def _shape(x):
     return x.shape
 
 
-def _data(name, a, x, shape):
-    """`a` as [T, B, X] data that goes with x: contiguous behind the second axis."""
-    if a.dtype != x.dtype or a.device != x.device or a.shape != shape:
-        raise ValueError(f"{name} must be a {x.dtype} tensor of shape {tuple(shape)} on {x.device}")
+def _rows(a):
+    """`a` with the axes behind the second contiguous."""
+    if a.is_contiguous():
+        return a
     n = 1
-    for size, step in zip(reversed(shape[2:]), reversed(a.stride()[2:])):
+    for size, step in zip(reversed(a.shape[2:]), reversed(a.stride()[2:])):
         if size != 1 and step != n:
             return a.contiguous()
         n *= size
     return a
 
 
+def _data(name, a, x, shape):
+    """`a` as [T, B, X] data that goes with x."""
+    if a.dtype != x.dtype or a.shape != shape or a.get_device() != x.get_device():
+        raise ValueError(f"{name} must be a {x.dtype} tensor of shape {tuple(shape)} on {x.device}")
+    return _rows(a)
+
+
 def _dense(name, a, x, shape, dtype=torch.float32):
-    if a is None:
-        return None
-    if a.dtype != dtype or a.device != x.device or a.shape != shape or not a.is_contiguous():
+    if a is not None and (a.dtype != dtype or a.shape != shape or not a.is_contiguous()
+                          or a.get_device() != x.get_device()):
         raise ValueError(f"{name} must be a contiguous {dtype} tensor of shape {tuple(shape)} on {x.device}")
-    return a
-
-
-def _like(x, shape=None):
-    """Uninitialised data of the given shape, time-major or batch-major as x is."""
-    shape = x.shape if shape is None else shape
-    if x.stride(0) < x.stride(1) and shape[0] > 1 and shape[1] > 1:
-        return torch.empty((shape[1], shape[0], *shape[2:]), dtype=x.dtype, device=x.device).transpose(0, 1)
-    return torch.empty(shape, dtype=x.dtype, device=x.device)
 
 
 def _bytes(n, x):
-    return torch.empty(n, dtype=torch.uint8, device=x.device) if n else None
+    return x.new_empty(n, dtype=torch.uint8) if n else None
 
 
 def _params(shape, x, empty):
@@ -97,12 +97,12 @@ def _conv_args(x, weight, bias, act, state, lengths):
     if weight.dim() != 2 or act not in ACTS:
         raise ValueError("weight must be [F, W], act None or 'silu'")
     W = weight.shape[1]
-    x = _data("x", x, x, (T, B, F))
+    x = _rows(x)
     _dense("weight", weight, x, (F, W))
     _dense("bias", bias, x, (F,))
     _dense("state", state, x, (W - 1, B, F), x.dtype)
     _dense("lengths", lengths, x, (B,), torch.int32)
-    return x, T, B, F, W, native.snn_conv_cfg(IO_OF[x.dtype], W, ACTS[act])
+    return x, T, B, F, W, _conv_cfg(IO_OF[x.dtype], W, ACTS[act])
 
 
 @_on_stream
@@ -112,7 +112,7 @@ def conv_forward(x, weight, bias=None, *, act="silu", state=None, state_out=None
     step 0; state_out: written with the last W-1 inputs, may be `state` (in place)."""
     x, T, B, F, W, cfg = _conv_args(x, weight, bias, act, state, lengths)
     _dense("state_out", state_out, x, (W - 1, B, F), x.dtype)
-    y = _like(x)
+    y = torch.empty_like(x)
     if x.numel():
         native.snn_conv_forward(cfg, T, B, F, x, weight, bias, state, lengths, y, state_out)
     else:
@@ -128,7 +128,7 @@ def conv_backward(x, weight, bias, grad_y, *, act="silu", state=None, lengths=No
     gy = _data("grad_y", grad_y, x, (T, B, F))
     _dense("grad_state_out", grad_state_out, x, (W - 1, B, F), x.dtype)
     empty = not x.numel()
-    gx, gw = _like(x), _params((F, W), x, empty)
+    gx, gw = torch.empty_like(x), _params((F, W), x, empty)
     gb = None if bias is None else _params((F,), x, empty)
     gs = None if state is None else torch.empty_like(state)
     if empty:
@@ -146,14 +146,14 @@ def _scan_args(x, dt, A, Bm, Cm, D, dt_bias, softplus, h_in, lengths):
     if Bm.dim() != 4 or A.dim() != 2:
         raise ValueError("A must be [F, S], Bm and Cm [T, B, G, S]")
     G, S = Bm.shape[2:]
-    x, dt = _data("x", x, x, (T, B, F)), _data("dt", dt, x, (T, B, F))
+    x, dt = _rows(x), _data("dt", dt, x, (T, B, F))
     Bm, Cm = _data("Bm", Bm, x, (T, B, G, S)), _data("Cm", Cm, x, (T, B, G, S))
     _dense("A", A, x, (F, S))
     _dense("D", D, x, (F,))
     _dense("dt_bias", dt_bias, x, (F,))
     _dense("h_in", h_in, x, (B, F, S))
     _dense("lengths", lengths, x, (B,), torch.int32)
-    cfg = native.snn_scan_cfg(IO_OF[x.dtype], S, G, int(bool(softplus)))
+    cfg = _scan_cfg(IO_OF[x.dtype], S, G, int(bool(softplus)))
     return (x, dt, A, Bm, Cm, D, dt_bias, h_in, lengths), (T, B, F, G, S), cfg
 
 
@@ -170,8 +170,8 @@ def scan_forward(x, dt, A, Bm, Cm, D=None, dt_bias=None, *, softplus=True, h_in=
     _dense("h_out", h_out, x, (B, F, S))
     if train and h_out is not None and h_out is h_in:
         raise ValueError("the backward reads h_in: h_out must be another tensor")
-    y = _like(x)
-    saved = torch.empty(native.snn_scan_saved_bytes(cfg, T, B, F), dtype=torch.uint8, device=x.device) if train else None
+    y = torch.empty_like(x)
+    saved = x.new_empty(native.snn_scan_saved_bytes(cfg, T, B, F), dtype=torch.uint8) if train else None
     if x.numel():
         ws = _bytes(native.snn_scan_workspace_bytes(cfg, T, B, F)[0], x)
         native.snn_scan_forward(cfg, T, B, F, *args, y, h_out, saved if train and saved.numel() else None, ws)
@@ -192,7 +192,7 @@ def scan_backward(x, dt, A, Bm, Cm, D, dt_bias, saved, grad_y, *, softplus=True,
     gy = _data("grad_y", grad_y, x, (T, B, F))
     _dense("grad_h_out", grad_h_out, x, (B, F, S))
     empty = not x.numel()
-    gx, gdt, gB, gC = _like(x), _like(x), _like(x, (T, B, G, S)), _like(x, (T, B, G, S))
+    gx, gdt, gB, gC = torch.empty_like(x), torch.empty_like(x), torch.empty_like(args[3]), torch.empty_like(args[4])
     gA = _params((F, S), x, empty)
     gD = None if D is None else _params((F,), x, empty)
     gbias = None if dt_bias is None else _params((F,), x, empty)
@@ -211,13 +211,13 @@ def scan_backward(x, dt, A, Bm, Cm, D, dt_bias, saved, grad_y, *, softplus=True,
 
 def _norm_args(y, r, z, w_post, scale, w_pre, eps, lengths):
     T, B, F = _shape(y)
-    y = _data("y", y, y, (T, B, F))
+    y = _rows(y)
     r = None if r is None else _data("r", r, y, (T, B, F))
     z = None if z is None else _data("z", z, y, (T, B, F))
     for name, w in (("w_post", w_post), ("scale", scale), ("w_pre", w_pre)):
         _dense(name, w, y, (F,))
     _dense("lengths", lengths, y, (B,), torch.int32)
-    return (y, z, r, w_post, scale, w_pre, lengths), (T, B, F), native.snn_norm_cfg(IO_OF[y.dtype], eps)
+    return (y, z, r, w_post, scale, w_pre, lengths), (T, B, F), _norm_cfg(IO_OF[y.dtype], eps)
 
 
 @_on_stream
@@ -227,7 +227,7 @@ def norm_forward(y, r=None, z=None, w_post=None, scale=None, w_pre=None, *, eps=
     weights w_post and w_pre.  Without z, w_post, scale, r or w_pre that part is left out.
     Returns (r_new, u or None, rstd), rstd for norm_backward with train=True, else None."""
     args, (T, B, F), cfg = _norm_args(y, r, z, w_post, scale, w_pre, eps, lengths)
-    r_new, u = _like(args[0]), None if w_pre is None else _like(args[0])
+    r_new, u = torch.empty_like(args[0]), None if w_pre is None else torch.empty_like(args[0])
     rstd = torch.empty((2, T, B), dtype=torch.float32, device=y.device) if train else None
     if y.numel():
         native.snn_norm_forward(cfg, T, B, F, *args, r_new, u, rstd)
@@ -244,7 +244,7 @@ def norm_backward(y, r, z, w_post, scale, w_pre, rstd, grad_r_new, grad_u=None, 
     g1 = None if grad_r_new is None else _data("grad_r_new", grad_r_new, y, (T, B, F))
     g2 = None if grad_u is None else _data("grad_u", grad_u, y, (T, B, F))
     empty = not y.numel()
-    gy, gr, gz = (None if a is None else _like(a) for a in (args[0], args[2], args[1]))
+    gy, gr, gz = (None if a is None else torch.empty_like(a) for a in (args[0], args[2], args[1]))
     gw = [None if w is None else _params((F,), y, empty) for w in (w_post, scale, w_pre)]
     if not empty:
         ws = _bytes(native.snn_norm_workspace_bytes(cfg, T, B, F), y)
