@@ -246,12 +246,15 @@ inline int norm_lanes(int64_t F) {
     return F > kNormRegs ? kBlock : int(ceil_div(F, kNormLane * kWave) * kWave);
 }
 
-// Workgroups walk rows g, g + groups, ...: parameters are read once and the backward keeps
-// one partial sum of their gradients.  16 waves per CU hide the latency of the sums.
-inline int64_t norm_groups(int64_t T, int64_t B, int64_t F) {
-    return std::min<int64_t>(T * B, ceil_div(256 * 16, norm_lanes(F) / kWave));
+// Workgroups walk rows g, g + groups, ..., so that parameters are read once.  The backward's
+// hold one partial sum of their gradients each, which 3 rows are to share at least (1250 rows of
+// 1537 fp32 features: 28 us with the sums joined, to 37 with 1 or 2, and 30 with 4).  Up to 32
+// waves per CU in the forward and 16 in the backward: whole rounds of the rows count for more.
+inline int64_t norm_groups(int64_t T, int64_t B, int64_t F, bool backward) {
+    const int64_t most = ceil_div(256 * (backward ? 16 : 32), norm_lanes(F) / kWave);
+    return std::min<int64_t>(backward ? ceil_div(T * B, 3) : T * B, most);
 }
-inline int64_t norm_workspace(int64_t T, int64_t B, int64_t F) { return piece(norm_groups(T, B, F) * 3 * F * 4); }
+inline int64_t norm_workspace(int64_t T, int64_t B, int64_t F) { return piece(norm_groups(T, B, F, true) * 3 * F * 4); }
 
 struct NormArgs {
     int64_t T, B, F;

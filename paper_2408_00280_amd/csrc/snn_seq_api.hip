@@ -83,7 +83,7 @@ snn_status check_scan_inputs(const snn_scan_cfg* c, int64_t T, int64_t B, int64_
 
 NormArgs norm_args(const snn_norm_cfg* c, int64_t T, int64_t B, int64_t F, const snn_seq* y, const snn_seq* z,
                    const snn_seq* r, const float* w_post, const float* scale, const float* w_pre,
-                   const int32_t* lengths) {
+                   const int32_t* lengths, bool backward) {
     NormArgs a = {};
     a.T = T;
     a.B = B;
@@ -96,7 +96,7 @@ NormArgs norm_args(const snn_norm_cfg* c, int64_t T, int64_t B, int64_t F, const
     a.scale = scale;
     a.w_pre = w_pre;
     a.lengths = lengths;
-    a.groups = norm_groups(T, B, F);
+    a.groups = norm_groups(T, B, F, backward);
     return a;
 }
 
@@ -266,7 +266,7 @@ snn_status snn_norm_forward(const snn_norm_cfg* cfg, int64_t T, int64_t B, int64
                       check_out(r_new, T, B, F, io), w_pre != nullptr ? check_out(u, T, B, F, io) : SNN_OK,
                       optional(rstd)});
     if (st != SNN_OK) return st;
-    NormArgs a = norm_args(cfg, T, B, F, y, z, r, w_post, scale, w_pre, lengths);
+    NormArgs a = norm_args(cfg, T, B, F, y, z, r, w_post, scale, w_pre, lengths, false);
     a.r_new = rows(r_new);
     a.u = rows(u);
     a.rstd = rstd;
@@ -299,7 +299,7 @@ snn_status snn_norm_backward(const snn_norm_cfg* cfg, int64_t T, int64_t B, int6
                       w_post != nullptr ? need(grad_w_post) : SNN_OK, scale != nullptr ? need(grad_scale) : SNN_OK,
                       w_pre != nullptr ? need(grad_w_pre) : SNN_OK, need(workspace, 16)});
     if (st != SNN_OK) return st;
-    NormArgs a = norm_args(cfg, T, B, F, y, z, r, w_post, scale, w_pre, lengths);
+    NormArgs a = norm_args(cfg, T, B, F, y, z, r, w_post, scale, w_pre, lengths, true);
     a.rstd_in = rstd;
     a.gr_new = rows(grad_r_new);
     a.gu = rows(grad_u);
