@@ -238,12 +238,12 @@ inline snn_status check_norm_cfg(const snn_norm_cfg* c) {
     return check_io(c->io) == SNN_OK && c->eps > 0.0f && std::isfinite(c->eps) ? SNN_OK : SNN_E_PARAM;
 }
 
-// Rows of up to 8192 features stay in registers, 8 features per lane; longer ones are read
-// again for each sum, by workgroups of kBlock lanes.
+// Rows of up to 8192 features stay in registers, 8 features per lane; longer ones are walked in
+// pieces of that.
 constexpr int kNormLane = 8, kNormRegs = 1024 * kNormLane;
 
 inline int norm_lanes(int64_t F) {
-    return F > kNormRegs ? kBlock : int(ceil_div(F, kNormLane * kWave) * kWave);
+    return int(ceil_div(std::min<int64_t>(F, kNormRegs), kNormLane * kWave) * kWave);
 }
 
 // Workgroups walk rows g, g + groups, ..., so that parameters are read once.  The backward's

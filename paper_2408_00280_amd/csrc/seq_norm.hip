@@ -4,151 +4,12 @@
 // Rows of up to 8192 features are read once: a lane holds 8 of a row's features (16 bytes of
 // bf16, two pieces of 16 bytes of fp32) and their parameters, a workgroup's lanes one row, and
 // the workgroup walks rows with the next one's loads in flight.  A row costs two sums over the
-// workgroup per direction, and more than one workgroup per CU hides them.  Longer rows go
-// through the plain kernels, which read the row again for each sum.  Bound by memory.
+// workgroup per direction, and more than one workgroup per CU hides them.  Longer rows are
+// walked in pieces and read again for each sum.  Bound by memory.
 #include "seq_device.h"
 
 namespace snnlif {
 namespace {
-
-// -- Long rows ---------------------------------------------------------------------------
-
-// Sum over the workgroup, in every lane.
-__device__ __forceinline__ float block_sum(float v, float* lds) {
-    v = wave_sum(v);
-    __syncthreads();
-    if ((threadIdx.x & (kWave - 1)) == 0) lds[threadIdx.x / kWave] = v;
-    __syncthreads();
-    float s = 0.0f;
-#pragma unroll
-    for (int w = 0; w < kBlock / kWave; ++w) s += lds[w];
-    return s;
-}
-
-template <int IO>
-struct NormRow {
-    const NormArgs& a;
-    int64_t t, b;
-    __device__ float gated(int64_t f) const {
-        const float y = load1<IO>(at<IO>(a.y, t, b, f));
-        if (a.z.p == nullptr) return y;
-        const float z = load1<IO>(at<IO>(a.z, t, b, f));
-        return y * (z * sigmoid(z));
-    }
-    __device__ float residual(int64_t f, float g, float k1) const {
-        const float n = a.w_post != nullptr ? g * k1 * a.w_post[f] : g;
-        const float r = a.r.p != nullptr ? load1<IO>(at<IO>(a.r, t, b, f)) : 0.0f;
-        return a.scale != nullptr ? fmaf(a.scale[f], n, r) : r + n;
-    }
-};
-
-template <int IO>
-__global__ __launch_bounds__(kBlock) void norm_long_forward_kernel(NormArgs a) {
-    __shared__ float lds[kBlock / kWave];
-    const int64_t i = blockIdx.x;
-    const NormRow<IO> row = {a, i / a.B, i % a.B};
-    const int64_t t = row.t, b = row.b;
-    if (t >= steps_of(a.lengths, b, a.T)) {
-        for (int64_t f = threadIdx.x; f < a.F; f += kBlock) {
-            store1<IO>(at_out<IO>(a.r_new, t, b, f), 0.0f);
-            if (a.w_pre != nullptr) store1<IO>(at_out<IO>(a.u, t, b, f), 0.0f);
-        }
-        return;
-    }
-    float k1 = 0.0f, k2 = 0.0f;
-    if (a.w_post != nullptr) {
-        float s = 0.0f;
-        for (int64_t f = threadIdx.x; f < a.F; f += kBlock) {
-            const float g = row.gated(f);
-            s = fmaf(g, g, s);
-        }
-        k1 = 1.0f / sqrtf(block_sum(s, lds) / float(a.F) + a.eps);
-    }
-    float s = 0.0f;
-    for (int64_t f = threadIdx.x; f < a.F; f += kBlock) {
-        const float r = row.residual(f, row.gated(f), k1);
-        s = fmaf(r, r, s);
-    }
-    if (a.w_pre != nullptr) k2 = 1.0f / sqrtf(block_sum(s, lds) / float(a.F) + a.eps);
-    for (int64_t f = threadIdx.x; f < a.F; f += kBlock) {
-        const float r = row.residual(f, row.gated(f), k1);
-        store1<IO>(at_out<IO>(a.r_new, t, b, f), r);
-        if (a.w_pre != nullptr) store1<IO>(at_out<IO>(a.u, t, b, f), r * k2 * a.w_pre[f]);
-    }
-    if (a.rstd != nullptr && threadIdx.x == 0) {
-        a.rstd[i] = k1;
-        a.rstd[a.T * a.B + i] = k2;
-    }
-}
-
-// Per row: with rn = r' k2, t = dL/du w_pre:  dL/dr' = dL/dr_new + k2 (t - rn mean(t rn));
-// with gn = g k1, t = dL/dr' scale w_post:    dL/dg = k1 (t - gn mean(t gn)).
-template <int IO>
-__global__ __launch_bounds__(kBlock) void norm_long_backward_kernel(NormArgs a) {
-    __shared__ float lds[kBlock / kWave];
-    float* part = a.part + int64_t(blockIdx.x) * 3 * a.F;      // w_post, scale, w_pre
-    for (int64_t f = threadIdx.x; f < a.F; f += kBlock) part[f] = part[a.F + f] = part[2 * a.F + f] = 0.0f;
-    for (int64_t i = blockIdx.x; i < a.T * a.B; i += a.groups) {
-        const NormRow<IO> row = {a, i / a.B, i % a.B};
-        const int64_t t = row.t, b = row.b;
-        if (t >= steps_of(a.lengths, b, a.T)) {
-            for (int64_t f = threadIdx.x; f < a.F; f += kBlock) {
-                store1<IO>(at_out<IO>(a.gy, t, b, f), 0.0f);
-                if (a.z.p != nullptr) store1<IO>(at_out<IO>(a.gz, t, b, f), 0.0f);
-                if (a.r.p != nullptr) store1<IO>(at_out<IO>(a.gr, t, b, f), 0.0f);
-            }
-            continue;
-        }
-        const float k1 = a.w_post != nullptr ? a.rstd_in[i] : 0.0f;
-        const float k2 = a.w_pre != nullptr ? a.rstd_in[a.T * a.B + i] : 0.0f;
-        const bool pre = a.w_pre != nullptr && a.gu.p != nullptr;
-        float m2 = 0.0f, m1 = 0.0f;
-        if (pre) {
-            float s = 0.0f;
-            for (int64_t f = threadIdx.x; f < a.F; f += kBlock) {
-                const float rn = row.residual(f, row.gated(f), k1) * k2;
-                s = fmaf(load1<IO>(at<IO>(a.gu, t, b, f)) * a.w_pre[f], rn, s);
-            }
-            m2 = block_sum(s, lds) / float(a.F);
-        }
-        const auto grad_r = [&](int64_t f, float& gw_pre) {
-            float gr = a.gr_new.p != nullptr ? load1<IO>(at<IO>(a.gr_new, t, b, f)) : 0.0f;
-            gw_pre = 0.0f;
-            if (pre) {
-                const float rn = row.residual(f, row.gated(f), k1) * k2, gu = load1<IO>(at<IO>(a.gu, t, b, f));
-                gr = fmaf(k2, gu * a.w_pre[f] - rn * m2, gr);
-                gw_pre = gu * rn;
-            }
-            return gr;
-        };
-        if (a.w_post != nullptr) {
-            float s = 0.0f, unused;
-            for (int64_t f = threadIdx.x; f < a.F; f += kBlock) {
-                const float w = a.w_post[f] * (a.scale != nullptr ? a.scale[f] : 1.0f);
-                s = fmaf(grad_r(f, unused) * w, row.gated(f) * k1, s);
-            }
-            m1 = block_sum(s, lds) / float(a.F);
-        }
-        for (int64_t f = threadIdx.x; f < a.F; f += kBlock) {
-            float gw_pre;
-            const float gr = grad_r(f, gw_pre), g = row.gated(f), gn = g * k1;
-            const float gs = a.scale != nullptr ? gr * a.scale[f] : gr;      // dL/dn
-            const float gg = a.w_post != nullptr ? k1 * (gs * a.w_post[f] - gn * m1) : gs;
-            const float n = a.w_post != nullptr ? gn * a.w_post[f] : g;
-            part[f] = fmaf(gs, gn, part[f]);
-            part[a.F + f] = fmaf(gr, n, part[a.F + f]);
-            part[2 * a.F + f] += gw_pre;
-            if (a.r.p != nullptr) store1<IO>(at_out<IO>(a.gr, t, b, f), gr);
-            if (a.z.p == nullptr) {
-                store1<IO>(at_out<IO>(a.gy, t, b, f), gg);
-            } else {
-                const float z = load1<IO>(at<IO>(a.z, t, b, f)), s = sigmoid(z);
-                store1<IO>(at_out<IO>(a.gz, t, b, f), gg * load1<IO>(at<IO>(a.y, t, b, f)) * silu_slope(z, s));
-                store1<IO>(at_out<IO>(a.gy, t, b, f), gg * (z * s));
-            }
-        }
-    }
-}
 
 // -- Rows in registers ---------------------------------------------------------------------
 
@@ -162,10 +23,10 @@ struct Lane8 {
         raw v[N];
     };
     int f[N], n[N];     // first feature and how many
-    __device__ explicit Lane8(int64_t F) {
+    __device__ explicit Lane8(int64_t F, int first = 0) {
 #pragma unroll
         for (int c = 0; c < N; ++c) {
-            f[c] = int(c * blockDim.x + threadIdx.x) * V;
+            f[c] = first + int(c * blockDim.x + threadIdx.x) * V;
             n[c] = max(0, min(V, int(F) - f[c]));
         }
     }
@@ -187,6 +48,11 @@ struct Lane8 {
                 out.v[c] = __builtin_bit_cast(raw, u);
             }
         }
+    }
+    __device__ void load(const Rows& r, int64_t t, int64_t b, float (&v)[kNormLane]) const {
+        Raw raw;
+        load(r, t, b, raw);
+        get(raw, v);
     }
     __device__ void get(const Raw& r, float (&v)[kNormLane]) const {
 #pragma unroll
@@ -224,6 +90,14 @@ struct Lane8 {
                 for (int j = 0; j < V; ++j) v[c * V + j] = j < n[c] ? (p != nullptr ? p[f[c] + j] : other) : 0.0f;
             }
         }
+    }
+    // p += x y, of partial sums that this workgroup alone holds.
+    __device__ void add(float* p, const float (&x)[kNormLane], const float (&y)[kNormLane]) const {
+        float v[kNormLane];
+        params(p, 0.0f, v);
+#pragma unroll
+        for (int i = 0; i < kNormLane; ++i) v[i] = fmaf(x[i], y[i], v[i]);
+        put(p, v);
     }
     __device__ void put(float* p, const float (&v)[kNormLane]) const {
 #pragma unroll
@@ -333,8 +207,26 @@ __global__ __launch_bounds__(MAXT) void norm_backward_kernel(NormArgs a) {
     lane.params(a.w_post, 1.0f, w_post);
     lane.params(a.scale, 1.0f, scale);
     lane.params(a.w_pre, 0.0f, w_pre);
+    // 16 waves of one workgroup have no registers for the next row's loads and the sums: those
+    // are in LDS then, each lane's own (x[1024][8][8192] bf16: 289 us, 383 with spilled registers)
+    constexpr bool kAhead = MAXT < 1024;
+    __shared__ f32x4_t sums[kAhead ? 1 : 6][kAhead ? 1 : MAXT];
+    const auto open = [&](int k, float (&g)[kNormLane]) {
+        if (kAhead) return;
+        const f32x4_t x = sums[2 * k][threadIdx.x], y = sums[2 * k + 1][threadIdx.x];
+#pragma unroll
+        for (int j = 0; j < kNormLane; ++j) g[j] = j < 4 ? x[j & 3] : y[j & 3];
+    };
+    const auto close = [&](int k, const float (&g)[kNormLane]) {
+        if (kAhead) return;
+        sums[2 * k][threadIdx.x] = {g[0], g[1], g[2], g[3]};
+        sums[2 * k + 1][threadIdx.x] = {g[4], g[5], g[6], g[7]};
+    };
 #pragma unroll
     for (int j = 0; j < kNormLane; ++j) g_post[j] = g_scale[j] = g_pre[j] = 0.0f;
+    close(0, g_post);
+    close(1, g_scale);
+    close(2, g_pre);
     const float mean = 1.0f / float(a.F);
     const int rows = int(a.T * a.B), B = int(a.B);
     const bool pre = a.w_pre != nullptr && a.gu.p != nullptr;
@@ -356,8 +248,6 @@ __global__ __launch_bounds__(MAXT) void norm_backward_kernel(NormArgs a) {
         }
         if (a.w_post != nullptr) row.k1 = a.rstd_in[i];
     };
-    // the next row's loads have no registers beside 16 waves of one workgroup
-    constexpr bool kAhead = MAXT < 1024;
     if (kAhead) fetch(blockIdx.x);
     for (int i = blockIdx.x; i < rows; i += int(a.groups)) {
         const int t = i / B, b = i - t * B;
@@ -398,25 +288,35 @@ __global__ __launch_bounds__(MAXT) void norm_backward_kernel(NormArgs a) {
                 for (int j = 0; j < kNormLane; ++j) rn[j] = 0.0f;
             }
 #pragma unroll
+            for (int j = 0; j < kNormLane; ++j) rn[j] = k2 * fmaf(scale[j], gn[j] * w_post[j], rn[j]);
+            open(2, g_pre);
+#pragma unroll
             for (int j = 0; j < kNormLane; ++j) {
-                rn[j] = k2 * fmaf(scale[j], gn[j] * w_post[j], rn[j]);
                 g_pre[j] = fmaf(gu[j], rn[j], g_pre[j]);
                 gu[j] *= w_pre[j];
                 s = fmaf(gu[j], rn[j], s);
             }
+            close(2, g_pre);
             const float m = sum(s) * mean;
 #pragma unroll
             for (int j = 0; j < kNormLane; ++j) gr[j] = fmaf(k2, fmaf(-m, rn[j], gu[j]), gr[j]);
             s = 0.0f;
         }
         if (a.r.p != nullptr) lane.store(a.gr, t, b, gr);
+        open(1, g_scale);
 #pragma unroll
         for (int j = 0; j < kNormLane; ++j) {
             g_scale[j] = fmaf(gr[j], gn[j] * w_post[j], g_scale[j]);
             gr[j] *= scale[j];                                     // dL/dn
+        }
+        close(1, g_scale);
+        open(0, g_post);
+#pragma unroll
+        for (int j = 0; j < kNormLane; ++j) {
             g_post[j] = fmaf(gr[j], gn[j], g_post[j]);
             gr[j] *= w_post[j];
         }
+        close(0, g_post);
         if (a.w_post != nullptr) {
 #pragma unroll
             for (int j = 0; j < kNormLane; ++j) s = fmaf(gr[j], gn[j], s);
@@ -436,9 +336,200 @@ __global__ __launch_bounds__(MAXT) void norm_backward_kernel(NormArgs a) {
         lane.store(a.gy, t, b, gr);
     }
     float* part = a.part + int64_t(blockIdx.x) * 3 * a.F;
+    open(0, g_post);
     lane.put(part, g_post);
+    open(1, g_scale);
     lane.put(part + a.F, g_scale);
+    open(2, g_pre);
     lane.put(part + 2 * a.F, g_pre);
+}
+
+// -- Longer rows: in pieces of 8192 features, read again for each sum (from the L2, as a rule) --
+
+constexpr int kLongLanes = kNormRegs / kNormLane;
+
+template <int IO>
+struct LongRow {
+    using L = Lane8<IO>;
+    const NormArgs& a;
+    int t, b;
+    __device__ void gated(const L& lane, float (&g)[kNormLane]) const {
+        lane.load(a.y, t, b, g);
+        if (a.z.p == nullptr) return;
+        float z[kNormLane];
+        lane.load(a.z, t, b, z);
+#pragma unroll
+        for (int j = 0; j < kNormLane; ++j) g[j] *= z[j] * sigmoid(z[j]);
+    }
+    // r' from g, which becomes g k1 w_post.
+    __device__ void residual(const L& lane, float k1, float (&g)[kNormLane], float (&r)[kNormLane]) const {
+        float w[kNormLane];
+        lane.params(a.w_post, 1.0f, w);
+#pragma unroll
+        for (int j = 0; j < kNormLane; ++j) {
+            g[j] *= k1 * w[j];
+            r[j] = 0.0f;
+        }
+        if (a.r.p != nullptr) lane.load(a.r, t, b, r);
+        lane.params(a.scale, 1.0f, w);
+#pragma unroll
+        for (int j = 0; j < kNormLane; ++j) r[j] = fmaf(w[j], g[j], r[j]);
+    }
+};
+
+template <int IO>
+__global__ __launch_bounds__(kLongLanes) void norm_long_forward_kernel(NormArgs a) {
+    __shared__ float lds[2][16];
+    using L = Lane8<IO>;
+    RowSum sum{lds};
+    const int F = int(a.F), rows = int(a.T * a.B), B = int(a.B);
+    const float mean = 1.0f / float(a.F);
+    for (int i = blockIdx.x; i < rows; i += int(a.groups)) {
+        const LongRow<IO> row = {a, i / B, i % B};
+        float g[kNormLane], r[kNormLane], w[kNormLane], k1 = 1.0f, k2 = 0.0f, s = 0.0f;
+        const bool in = row.t < steps_of(a.lengths, row.b, a.T);
+        if (in && a.w_post != nullptr) {
+            for (int f = 0; f < F; f += kNormRegs) {
+                row.gated(L(F, f), g);
+#pragma unroll
+                for (int j = 0; j < kNormLane; ++j) s = fmaf(g[j], g[j], s);
+            }
+            k1 = 1.0f / sqrtf(fmaf(sum(s), mean, a.eps));
+        }
+        if (in && a.w_pre != nullptr) {
+            s = 0.0f;
+            for (int f = 0; f < F; f += kNormRegs) {
+                const L lane(F, f);
+                row.gated(lane, g);
+                row.residual(lane, k1, g, r);
+#pragma unroll
+                for (int j = 0; j < kNormLane; ++j) s = fmaf(r[j], r[j], s);
+            }
+            k2 = 1.0f / sqrtf(fmaf(sum(s), mean, a.eps));
+        }
+        for (int f = 0; f < F; f += kNormRegs) {
+            const L lane(F, f);
+            if (in) {
+                row.gated(lane, g);
+                row.residual(lane, k1, g, r);
+            } else {
+#pragma unroll
+                for (int j = 0; j < kNormLane; ++j) r[j] = 0.0f;
+            }
+            lane.store(a.r_new, row.t, row.b, r);
+            if (a.w_pre != nullptr) {
+                lane.params(a.w_pre, 0.0f, w);
+#pragma unroll
+                for (int j = 0; j < kNormLane; ++j) r[j] *= k2 * w[j];
+                lane.store(a.u, row.t, row.b, r);
+            }
+        }
+        if (in && a.rstd != nullptr && threadIdx.x == 0) {
+            a.rstd[i] = k1;
+            a.rstd[rows + i] = k2;
+        }
+    }
+}
+
+template <int IO>
+__global__ __launch_bounds__(kLongLanes) void norm_long_backward_kernel(NormArgs a) {
+    __shared__ float lds[2][16];
+    using L = Lane8<IO>;
+    RowSum sum{lds};
+    const int F = int(a.F), rows = int(a.T * a.B), B = int(a.B);
+    const float mean = 1.0f / float(a.F);
+    const bool pre = a.w_pre != nullptr && a.gu.p != nullptr;
+    float* part = a.part + int64_t(blockIdx.x) * 3 * a.F;      // w_post, scale, w_pre
+    const float zero[kNormLane] = {};
+    for (int k = 0; k < 3; ++k)
+        for (int f = 0; f < F; f += kNormRegs) L(F, f).put(part + k * a.F, zero);
+    for (int i = blockIdx.x; i < rows; i += int(a.groups)) {
+        const LongRow<IO> row = {a, i / B, i % B};
+        const int t = row.t, b = row.b;
+        if (t >= steps_of(a.lengths, b, a.T)) {
+            for (int f = 0; f < F; f += kNormRegs) {
+                const L lane(F, f);
+                lane.store(a.gy, t, b, zero);
+                if (a.z.p != nullptr) lane.store(a.gz, t, b, zero);
+                if (a.r.p != nullptr) lane.store(a.gr, t, b, zero);
+            }
+            continue;
+        }
+        const float k1 = a.w_post != nullptr ? a.rstd_in[i] : 1.0f, k2 = pre ? a.rstd_in[rows + i] : 0.0f;
+        float n[kNormLane], rn[kNormLane], gu[kNormLane], w[kNormLane], m2 = 0.0f, m1 = 0.0f, s = 0.0f;
+        if (pre) {
+            for (int f = 0; f < F; f += kNormRegs) {
+                const L lane(F, f);
+                row.gated(lane, n);
+                row.residual(lane, k1, n, rn);
+                lane.load(a.gu, t, b, gu);
+                lane.params(a.w_pre, 0.0f, w);
+#pragma unroll
+                for (int j = 0; j < kNormLane; ++j) s = fmaf(gu[j] * w[j], rn[j] * k2, s);
+            }
+            m2 = sum(s) * mean;
+        }
+        // dL/dr', and n and r' k2 beside it
+        const auto grad_r = [&](const L& lane, float (&gr)[kNormLane]) {
+            row.gated(lane, n);
+            row.residual(lane, k1, n, rn);
+#pragma unroll
+            for (int j = 0; j < kNormLane; ++j) gr[j] = 0.0f;
+            if (a.gr_new.p != nullptr) lane.load(a.gr_new, t, b, gr);
+            if (!pre) return;
+            lane.load(a.gu, t, b, gu);
+            lane.params(a.w_pre, 0.0f, w);
+#pragma unroll
+            for (int j = 0; j < kNormLane; ++j) {
+                rn[j] *= k2;
+                gr[j] = fmaf(k2, fmaf(-m2, rn[j], gu[j] * w[j]), gr[j]);
+            }
+        };
+        float gr[kNormLane];
+        if (a.w_post != nullptr) {
+            s = 0.0f;
+            for (int f = 0; f < F; f += kNormRegs) {
+                const L lane(F, f);
+                grad_r(lane, gr);
+                lane.params(a.scale, 1.0f, w);
+#pragma unroll
+                for (int j = 0; j < kNormLane; ++j) s = fmaf(gr[j] * w[j], n[j], s);   // n = g k1 w_post
+            }
+            m1 = sum(s) * mean;
+        }
+        for (int f = 0; f < F; f += kNormRegs) {
+            const L lane(F, f);
+            grad_r(lane, gr);
+            if (a.r.p != nullptr) lane.store(a.gr, t, b, gr);
+            if (pre) lane.add(part + 2 * a.F, gu, rn);
+            lane.add(part + a.F, gr, n);
+            lane.params(a.scale, 1.0f, w);
+            float y[kNormLane], z[kNormLane], gn[kNormLane];
+            lane.load(a.y, t, b, y);
+            if (a.z.p != nullptr) lane.load(a.z, t, b, z);
+#pragma unroll
+            for (int j = 0; j < kNormLane; ++j) {
+                gr[j] *= w[j];                                     // dL/dn
+                gn[j] = y[j] * k1 * (a.z.p != nullptr ? z[j] * sigmoid(z[j]) : 1.0f);
+            }
+            if (a.w_post != nullptr) {
+                lane.add(part, gr, gn);
+                lane.params(a.w_post, 1.0f, w);
+#pragma unroll
+                for (int j = 0; j < kNormLane; ++j) gr[j] = k1 * fmaf(-m1, gn[j], gr[j] * w[j]);   // dL/dg
+            }
+            if (a.z.p != nullptr) {
+#pragma unroll
+                for (int j = 0; j < kNormLane; ++j) {
+                    const float q = sigmoid(z[j]);
+                    y[j] *= gr[j] * silu_slope(z[j], q);
+                    gr[j] *= z[j] * q;
+                }
+                lane.store(a.gz, t, b, y);
+            }
+            lane.store(a.gy, t, b, gr);
+        }
+    }
 }
 
 // 64 values per workgroup, its waves over the partial results.
@@ -471,8 +562,8 @@ snn_status reduce_entry(const float* part, int64_t P, int64_t stride, const Redu
 
 template <int IO>
 static snn_status norm_forward_io(const NormArgs& a, hipStream_t s) {
-    if (a.F > kNormRegs) return launch(norm_long_forward_kernel<IO>, dim3(unsigned(a.T * a.B)), s, a);
     const dim3 grid{unsigned(a.groups)};
+    if (a.F > kNormRegs) return launch_blk(norm_long_forward_kernel<IO>, grid, kLongLanes, s, a);
     const int n = norm_lanes(a.F);
     return n > 512 ? launch_blk(norm_forward_kernel<IO, 1024>, grid, n, s, a)
                    : launch_blk(norm_forward_kernel<IO, 512>, grid, n, s, a);
@@ -481,7 +572,7 @@ static snn_status norm_forward_io(const NormArgs& a, hipStream_t s) {
 template <int IO>
 static snn_status norm_backward_io(const NormArgs& a, hipStream_t s) {
     const dim3 grid{unsigned(a.groups)};
-    if (a.F > kNormRegs) return launch(norm_long_backward_kernel<IO>, grid, s, a);
+    if (a.F > kNormRegs) return launch_blk(norm_long_backward_kernel<IO>, grid, kLongLanes, s, a);
     const int n = norm_lanes(a.F);
     return n > 512 ? launch_blk(norm_backward_kernel<IO, 1024>, grid, n, s, a)
                    : launch_blk(norm_backward_kernel<IO, 512>, grid, n, s, a);
