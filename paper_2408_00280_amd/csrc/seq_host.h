@@ -148,7 +148,7 @@ inline snn_status check_scan_cfg(const snn_scan_cfg* c) {
 
 constexpr int kScanStates = 4;   // states per lane
 constexpr int kScanBlock = 8;    // steps that the waves of the local pass share out at a time
-constexpr int64_t kSplitWaves = 1024, kSplitSteps = 128, kMaxSegments = 1024;
+constexpr int64_t kSplitWaves = 1024, kSplitGroups = 128, kSplitSteps = 128, kMaxSegments = 1024;
 
 // A workgroup owns 64 features of one group and one sequence, a feature per lane; each of its
 // `waves` (a power of two) waves holds 4 of their states.  The forward keeps the state every
@@ -168,10 +168,11 @@ constexpr int scan_keep(int waves) { return waves == 4 || waves == 8 ? 16 : 8; }
 constexpr int64_t scan_held_states(int S) { return int64_t(S + kScanStates - 1) / kScanStates * kScanStates; }
 
 // The time axis is cut into segments where the waves of one segment leave SIMDs (1024 of them)
-// without two waves: the local pass then costs less than the idle SIMDs (x[1024][8][4096], with
-// two, gains nothing from it; x[4096][1][4096] runs in 160 us instead of 624).  Four waves per
-// SIMD are aimed for, with segments of 16 steps or more (x[333][5][777] of 7 states: forward
-// and backward in 79 us, 114 with 64 or more), once the steps outweigh two more launches.
+// without two waves, or its workgroups half the CUs without one: the local pass then costs less
+// than they do idle (x[4096][1][4096] runs in 160 us instead of 624; x[1024][8][4096], which has
+// two waves per SIMD, gains nothing).  Four waves per SIMD are aimed for, with segments of 16
+// steps or more (x[333][5][777] of 7 states: forward and backward in 79 us, 114 with 64 or
+// more), once the steps outweigh two more launches.
 inline ScanPlan scan_plan(const snn_scan_cfg* c, int64_t T, int64_t B, int64_t F) {
     ScanPlan p;
     p.waves = 1;
@@ -180,9 +181,9 @@ inline ScanPlan scan_plan(const snn_scan_cfg* c, int64_t T, int64_t B, int64_t F
     p.tiles = ceil_div(F / c->groups, kWave);
     p.steps = std::max<int64_t>(T, 1);
     p.segments = 1;
-    const int64_t waves = p.tiles * c->groups * B * (scan_held_states(c->states) / kScanStates);
-    const int64_t want = std::min(std::min<int64_t>(4096 / waves, T / 16), int64_t(kMaxSegments));
-    if (waves <= kSplitWaves && T >= kSplitSteps && want > 1) {
+    const int64_t groups = p.tiles * c->groups * B, waves = groups * (scan_held_states(c->states) / kScanStates);
+    const int64_t want = std::min(std::min(std::max<int64_t>(4096 / waves, 2), T / 16), kMaxSegments);
+    if ((waves <= kSplitWaves || groups <= kSplitGroups) && T >= kSplitSteps && want > 1) {
         p.steps = ceil_div(ceil_div(T, want), 16) * 16;      // whole blocks, in either direction
         p.segments = ceil_div(T, p.steps);
     }

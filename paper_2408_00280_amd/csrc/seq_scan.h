@@ -36,7 +36,10 @@ __device__ __forceinline__ ScanPlace scan_place(const ScanArgs& a, int first_seg
     return p;
 }
 
-// A[f][n] log2(e) of the lane's states, 0 behind the last (whose state then stays 0).
+// Where S is not whole lanes (FULL = false in the kernels), the last wave leaves its states
+// behind the last one out of its sums: B = C = 0 there, which gives 0 with finite values only.
+
+// A[f][n] log2(e) of the lane's states, 0 behind the last.
 __device__ __forceinline__ void load_rates(const ScanArgs& a, const ScanPlace& p, float (&r)[kSL]) {
 #pragma unroll
     for (int i = 0; i < kSL; ++i) r[i] = i < p.states ? a.A[p.f * a.S + p.first + i] * kLog2e : 0.0f;

@@ -51,16 +51,25 @@ struct BackwardLds {
     float sgbc[K][NS][2 * kSL];  // dL/dB and dL/dC
 };
 
-template <int IO, int NS>
+template <int IO, int NS, bool FULL>
 __global__ __launch_bounds__(NS * kWave, NS > 8 ? 4 : 2) void scan_backward_kernel(ScanArgs a) {
     constexpr int K = scan_keep(NS), R = K > NS ? K / NS : 1;
+    // 4 waves per SIMD need no step read ahead, and have no registers for it
+    constexpr bool kAhead = NS <= 8;
     extern __shared__ __align__(16) char lds[];
     auto& m = *reinterpret_cast<BackwardLds<NS>*>(lds);
     const ScanPlace p = scan_place(a);
     float rate[kSL], e[kSL], gA[kSL], gD = 0.0f, gbias = 0.0f;
     load_rates(a, p, rate);
-    if (a.plan.segments == 1) load_state(a, p, a.gh_out, e);
-    else if (p.states > 0) StateColumn(a, p, a.part_h).load(blockIdx.y, e);
+    // Lanes behind the group's last feature have steps and states of 0 and add nothing.
+    const auto load = [&](const float* first, const StateColumn& kept, int64_t c, bool at_first, float (&v)[kSL]) {
+#pragma unroll
+        for (int s = 0; s < kSL; ++s) v[s] = 0.0f;
+        if (!p.active) return;
+        if (at_first) load_state(a, p, first, v);
+        else if (p.states > 0) kept.load(c, v);
+    };
+    load(a.gh_out, StateColumn(a, p, a.part_h), blockIdx.y, a.plan.segments == 1, e);
 #pragma unroll
     for (int i = 0; i < kSL; ++i) gA[i] = 0.0f;
     const float skip = a.D != nullptr ? a.D[p.f] : 0.0f, bias = a.dt_bias != nullptr ? a.dt_bias[p.f] : 0.0f;
@@ -89,11 +98,8 @@ __global__ __launch_bounds__(NS * kWave, NS > 8 ? 4 : 2) void scan_backward_kern
                 const float v = IoVec<IO, 1>::get(raw[r].dt, 0) + bias, x = IoVec<IO, 1>::get(raw[r].x, 0);
                 mine[r][0] = x;
                 mine[r][1] = 1.0f;
-                d.d = a.softplus ? softplus(v, mine[r][1]) : v;
-                if (p.active) {                  // lanes behind the group add nothing
-                    d.dx = d.d * x;
-                    d.gy = IoVec<IO, 1>::get(raw[r].gy, 0);
-                }
+                const float step = a.softplus ? softplus(v, mine[r][1]) : v;
+                if (p.active) d = {step, step * x, IoVec<IO, 1>::get(raw[r].gy, 0)};
             }
             if (k < K) m.sd[to][k][p.lane] = d;
         }
@@ -130,8 +136,7 @@ __global__ __launch_bounds__(NS * kWave, NS > 8 ? 4 : 2) void scan_backward_kern
         const f32x4_t* bc = reinterpret_cast<const f32x4_t*>(m.sbc[block].v[k][p.wave]);
         return Ahead{m.sd[block][k][p.lane], bc[0], bc[1]};
     };
-    if (t0 > 0 && busy) kept.load(t0 / K - 1, h);
-    else load_state(a, p, a.h_in, h);
+    load(a.h_in, kept, t0 / K - 1, t0 <= 0, h);
     lds_barrier();
     int buf = 0;
     for (; t0 >= p.t0; t0 -= K) {
@@ -143,7 +148,8 @@ __global__ __launch_bounds__(NS * kWave, NS > 8 ? 4 : 2) void scan_backward_kern
             for (int s = 0; s < kSL; ++s) hs[0][s] = h[s];
 #pragma unroll
             for (int k = 0; k < K; ++k) {
-                if (k + 1 < K) ahead = read(buf, k + 1);
+                if (kAhead && k + 1 < K) ahead = read(buf, k + 1);
+                if (!kAhead) step = read(buf, k);
                 __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
                 for (int s = 0; s < kSL; ++s) {
@@ -151,7 +157,7 @@ __global__ __launch_bounds__(NS * kWave, NS > 8 ? 4 : 2) void scan_backward_kern
                     hs[k + 1][s] = fmaf(dec[k][s], hs[k][s], step.d.dx * step.b[s]);
                 }
                 __builtin_amdgcn_sched_barrier(0);
-                if (k + 1 < K) step = ahead;
+                if (kAhead && k + 1 < K) step = ahead;
             }
             // the sums over the wave run a step behind, beside the next step's recurrence
             float v[2 * kSL];
@@ -160,10 +166,10 @@ __global__ __launch_bounds__(NS * kWave, NS > 8 ? 4 : 2) void scan_backward_kern
             };
 #pragma unroll
             for (int k = K - 1; k >= 0; --k) {
-                if (k > 0) ahead = read(buf, k - 1);
+                if (kAhead && k > 0) ahead = read(buf, k - 1);
+                if (!kAhead) step = read(buf, k);
                 if (k == K / 2) {                // half of the block's registers are free by now
-                    if (below > 0) kept.load(below / K - 1, h_next);
-                    else load_state(a, p, a.h_in, h_next);
+                    load(a.h_in, kept, below / K - 1, below == 0, h_next);
                 }
                 __builtin_amdgcn_sched_barrier(0);
                 if (k < K - 1) sum_up(k + 1);
@@ -174,15 +180,16 @@ __global__ __launch_bounds__(NS * kWave, NS > 8 ? 4 : 2) void scan_backward_kern
                     const float b = step.b[s], dh = fmaf(step.c[s], d.gy, e[s]);
                     v[s] = dh * d.dx;
                     v[kSL + s] = d.gy * hs[k + 1][s];
-                    gx = fmaf(dh, b, gx);
+                    const bool in = FULL || s < p.states;
+                    gx = in ? fmaf(dh, b, gx) : gx;
                     e[s] = dec[k][s] * dh;
                     const float q = e[s] * hs[k][s];
-                    gd = fmaf(q, rate[s], gd);
+                    gd = in ? fmaf(q, rate[s], gd) : gd;
                     gA[s] = fmaf(q, d.d, gA[s]);
                 }
                 m.sg[p.wave][k][p.lane] = {gx, gd};
                 __builtin_amdgcn_sched_barrier(0);
-                step = ahead;
+                if (kAhead) step = ahead;
             }
             sum_up(0);
 #pragma unroll
@@ -208,7 +215,7 @@ __global__ __launch_bounds__(NS * kWave, NS > 8 ? 4 : 2) void scan_backward_kern
                         db += w < used ? g[w].x : 0.0f;
                         da += w < used ? g[w].y : 0.0f;
                     }
-                    gx = fmaf(s.d, db, skip * s.gy);
+                    gx = fmaf(s.d, db, a.D != nullptr ? skip * s.gy : 0.0f);
                     const float x = own[r][0];
                     gdt = fmaf(x, db, da * kLn2) * own[r][1];    // rate is A log2 e
                     gD = fmaf(s.gy, x, gD);
@@ -268,26 +275,30 @@ __global__ __launch_bounds__(kBlock) void scan_join_kernel(ScanArgs a, int64_t n
     store1<IO>(at_out<IO>(which ? a.gC : a.gB, t, b, g * a.S + s), sum);
 }
 
-template <int IO, int NS>
+template <int IO, int NS, bool FULL>
 snn_status backward_launch(const ScanArgs& a, hipStream_t s) {
     ScanArgs arg = a;
     void* argv[] = {&arg};
     const dim3 grid(unsigned(a.plan.tiles * a.G * a.B), unsigned(a.plan.segments));
-    const hipError_t e = hipLaunchKernel(reinterpret_cast<const void*>(scan_backward_kernel<IO, NS>), grid,
+    const hipError_t e = hipLaunchKernel(reinterpret_cast<const void*>(scan_backward_kernel<IO, NS, FULL>), grid,
                                          dim3(NS * kWave), argv, sizeof(BackwardLds<NS>), s);
     return e == hipSuccess ? SNN_OK : SNN_E_LAUNCH;
 }
 
+template <int IO, bool FULL>
+snn_status backward_states(const ScanArgs& a, hipStream_t s) {
+    switch (a.plan.waves) {
+        case 1: return backward_launch<IO, 1, FULL>(a, s);
+        case 2: return backward_launch<IO, 2, FULL>(a, s);
+        case 4: return backward_launch<IO, 4, FULL>(a, s);
+        case 8: return backward_launch<IO, 8, FULL>(a, s);
+        default: return backward_launch<IO, 16, FULL>(a, s);
+    }
+}
+
 template <int IO>
 snn_status backward_io(const ScanArgs& a, hipStream_t s) {
-    snn_status st;
-    switch (a.plan.waves) {
-        case 1: st = backward_launch<IO, 1>(a, s); break;
-        case 2: st = backward_launch<IO, 2>(a, s); break;
-        case 4: st = backward_launch<IO, 4>(a, s); break;
-        case 8: st = backward_launch<IO, 8>(a, s); break;
-        default: st = backward_launch<IO, 16>(a, s); break;
-    }
+    snn_status st = a.S % kSL == 0 ? backward_states<IO, true>(a, s) : backward_states<IO, false>(a, s);
     if (st != SNN_OK) return st;
     const int64_t n = a.T * a.B * a.G * 2 * a.S;
     if ((st = launch(scan_join_kernel<IO>, grid_for(n), s, a, n)) != SNN_OK) return st;

@@ -13,7 +13,7 @@
 namespace snnlif {
 namespace {
 
-template <int IO, int NS, int K>
+template <int IO, int NS, int K, bool FULL>
 __global__ __launch_bounds__(NS * kWave) void scan_forward_kernel(ScanArgs a) {
     constexpr int R = K > NS ? K / NS : 1, U = 2;   // U: steps read from LDS ahead
     __shared__ float2 sd[3][K][kWave];           // (d, d x): of this block, the next and the one being staged
@@ -55,7 +55,7 @@ __global__ __launch_bounds__(NS * kWave) void scan_forward_kernel(ScanArgs a) {
                 const float v = IoVec<IO, 1>::get(dr[r], 0) + bias, x = IoVec<IO, 1>::get(xr[r], 0);
                 d.x = a.softplus ? softplus(v) : v;
                 d.y = d.x * x;
-                skipped[r] = skip * x;
+                skipped[r] = a.D != nullptr ? skip * x : 0.0f;
             }
             if (k < K) sd[to][k][p.lane] = d;
         }
@@ -98,7 +98,7 @@ __global__ __launch_bounds__(NS * kWave) void scan_forward_kernel(ScanArgs a) {
 #pragma unroll
                         for (int s = 0; s < kSL; ++s) {
                             h[s] = fmaf(__builtin_amdgcn_exp2f(step[i].d.x * rate[s]), h[s], step[i].d.y * step[i].b[s]);
-                            y = fmaf(step[i].c[s], h[s], y);
+                            y = FULL || s < p.states ? fmaf(step[i].c[s], h[s], y) : y;
                         }
                         sy[buf][p.wave][u + i][p.lane] = y;
                     }
@@ -129,6 +129,71 @@ __global__ __launch_bounds__(NS * kWave) void scan_forward_kernel(ScanArgs a) {
         }
         now = next;
         buf ^= 1;
+    }
+    if (a.h_out != nullptr && p.t1 == a.T) store_state(a, p, a.h_out, h);
+}
+
+// Up to 4 states: one wave holds them all, so that steps and sums need no LDS and only B and C
+// go through it; without the LDS of the shared form four times as many waves fit a CU.
+template <int IO, bool FULL>
+__global__ __launch_bounds__(kWave) void scan_forward_one_kernel(ScanArgs a) {
+    constexpr int K = 8;
+    __shared__ __align__(16) StagedBC<1, K> sbc[2];
+    const ScanPlace p = scan_place(a);
+    float rate[kSL], h[kSL];
+    load_rates(a, p, rate);
+    if (a.plan.segments == 1) load_state(a, p, a.h_in, h);
+    else StateColumn(a, p, a.part_h).load(blockIdx.y, h);
+    const float skip = a.D != nullptr ? a.D[p.f] : 0.0f, bias = a.dt_bias != nullptr ? a.dt_bias[p.f] : 0.0f;
+    const Columns<IO> cx(a.x, p), cdt(a.dt, p), cy(a.y, p);
+    const StateColumn kept(a, p, a.saved);
+    BCColumns<IO, 1, K> cbc(a, p, p.t0);
+    typename IoVec<IO, 1>::raw xr[K], dr[K];
+    const auto fetch = [&](int t0) {
+        cbc.template fetch<1>(t0, p.t0, p.len);
+#pragma unroll
+        for (int k = 0; k < K; ++k) {
+            if (t0 + k < p.len) {
+                xr[k] = cx.load(t0 + k);
+                dr[k] = cdt.load(t0 + k);
+            }
+        }
+    };
+    fetch(p.t0);
+    int buf = 0;
+    for (int t0 = p.t0; t0 < p.t1; t0 += K, buf ^= 1) {
+        const int n = min(K, p.len - t0);                        // steps inside the sequence
+        if (n > 0) {
+            if (a.saved != nullptr && t0 > 0 && (t0 & (a.plan.keep - 1)) == 0 && p.active)
+                kept.store(t0 / a.plan.keep - 1, h);
+            float x[K], d[K];
+#pragma unroll
+            for (int k = 0; k < K; ++k) {
+                x[k] = d[k] = 0.0f;                              // behind the end: the state stays
+                if (k < n) {
+                    const float v = IoVec<IO, 1>::get(dr[k], 0) + bias;
+                    x[k] = IoVec<IO, 1>::get(xr[k], 0);
+                    d[k] = a.softplus ? softplus(v) : v;
+                }
+            }
+            cbc.stage(t0, p.len, sbc[buf]);
+            fetch(t0 + K);
+            lds_barrier();
+            const f32x4_t* bc = reinterpret_cast<const f32x4_t*>(sbc[buf].v[0][0]);
+#pragma unroll
+            for (int k = 0; k < K; ++k) {
+                const f32x4_t b = bc[2 * k], c = bc[2 * k + 1];
+                float y = a.D != nullptr ? skip * x[k] : 0.0f;
+#pragma unroll
+                for (int s = 0; s < kSL; ++s) {
+                    h[s] = fmaf(__builtin_amdgcn_exp2f(d[k] * rate[s]), h[s], (d[k] * x[k]) * b[s]);
+                    y = FULL || s < p.states ? fmaf(c[s], h[s], y) : y;
+                }
+                if (k < n && p.active) cy.store(t0 + k, y);
+            }
+        }
+        for (int k = max(n, 0); k < K && t0 + k < p.t1; ++k)
+            if (p.active) cy.store(t0 + k, 0.0f);
     }
     if (a.h_out != nullptr && p.t1 == a.T) store_state(a, p, a.h_out, h);
 }
@@ -193,9 +258,9 @@ __global__ __launch_bounds__(kBlock) void scan_token_kernel(ScanArgs a) {
 #pragma unroll
             for (int j = 0; j < kSL; ++j) {
                 h[k][j] = fmaf(__builtin_amdgcn_exp2f(d * (rate[j] * kLog2e)), h[k][j], (d * x[k]) * bv[k][j]);
-                y = fmaf(cv[k][j], h[k][j], y);
+                y = j < states ? fmaf(cv[k][j], h[k][j], y) : y;
             }
-            y = q == 0 ? fmaf(skip, x[k], y) : y;
+            y = q == 0 && a.D != nullptr ? fmaf(skip, x[k], y) : y;
         }
         if (Q > 1) y += dpp<kDppXor1>(y);
         if (Q > 2) y += dpp<kDppXor2>(y);
@@ -236,29 +301,36 @@ snn_status token_states(const ScanArgs& a, hipStream_t s) {
     }
 }
 
-template <int IO, int NS>
+template <int IO, int NS, bool FULL>
 snn_status forward_waves(const ScanArgs& a, hipStream_t s) {
     const dim3 grid(unsigned(a.plan.tiles * a.G * a.B), unsigned(a.plan.segments));
+    if constexpr (NS == 1) return launch_blk(scan_forward_one_kernel<IO, FULL>, grid, kWave, s, a);
     // Up to two workgroups of four waves per CU have the LDS for blocks of 16 steps, whose
     // barriers are half as many (x[1024][8][4096]: 218 us to 244 with blocks of 8); more of
     // them hide the barriers themselves and need blocks of 8 to fit (x[4096][1][4096] in 16
     // segments: 88 us to 103 with blocks of 16).
     if constexpr (NS == 4) {
-        if (int64_t(grid.x) * grid.y <= 2 * 256) return launch_blk(scan_forward_kernel<IO, NS, 16>, grid, NS * kWave, s, a);
+        if (int64_t(grid.x) * grid.y <= 2 * 256)
+            return launch_blk(scan_forward_kernel<IO, NS, 16, FULL>, grid, NS * kWave, s, a);
     }
-    return launch_blk(scan_forward_kernel<IO, NS, 8>, grid, NS * kWave, s, a);
+    if constexpr (NS > 1) return launch_blk(scan_forward_kernel<IO, NS, 8, FULL>, grid, NS * kWave, s, a);
+}
+
+template <int IO, bool FULL>
+snn_status forward_states(const ScanArgs& a, hipStream_t s) {
+    switch (a.plan.waves) {
+        case 1: return forward_waves<IO, 1, FULL>(a, s);
+        case 2: return forward_waves<IO, 2, FULL>(a, s);
+        case 4: return forward_waves<IO, 4, FULL>(a, s);
+        case 8: return forward_waves<IO, 8, FULL>(a, s);
+        default: return forward_waves<IO, 16, FULL>(a, s);
+    }
 }
 
 template <int IO>
 snn_status forward_io(const ScanArgs& a, hipStream_t s) {
     if (a.T == 1) return token_states<IO>(a, s);
-    switch (a.plan.waves) {
-        case 1: return forward_waves<IO, 1>(a, s);
-        case 2: return forward_waves<IO, 2>(a, s);
-        case 4: return forward_waves<IO, 4>(a, s);
-        case 8: return forward_waves<IO, 8>(a, s);
-        default: return forward_waves<IO, 16>(a, s);
-    }
+    return a.S % kSL == 0 ? forward_states<IO, true>(a, s) : forward_states<IO, false>(a, s);
 }
 
 }  // namespace

@@ -114,6 +114,12 @@ __global__ __launch_bounds__(NS * kWave) void scan_local_kernel(ScanArgs a) {
     }
 }
 
+// A state that is not finite stays so over a segment, as it does step by step, where the decays
+// of a whole segment multiply to 0 in 32 bits.
+__device__ __forceinline__ float decayed(float decay, float h) {
+    return fabsf(h) < __builtin_inff() ? decay * h : h;
+}
+
 // A lane per sequence, state and feature walks the segments.  On return part_h[c] is the state
 // before segment c (or e behind it), and the last one goes to h_out (gh_in).
 template <bool DOWN>
@@ -140,7 +146,7 @@ __global__ __launch_bounds__(kBlock) void scan_carry_kernel(ScanArgs a, int64_t 
         for (int u = 0; u < U; ++u) {
             if (c0 + u < a.plan.segments) {
                 a.part_h[(DOWN ? a.plan.segments - 1 - c0 - u : c0 + u) * n + i] = h;
-                if (c0 + u + 1 < a.plan.segments) h = fmaf(__builtin_amdgcn_exp2f(d[u] * rate), h, local[u]);
+                if (c0 + u + 1 < a.plan.segments) h = decayed(__builtin_amdgcn_exp2f(d[u] * rate), h) + local[u];
             }
         }
     }

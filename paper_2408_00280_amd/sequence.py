@@ -168,7 +168,7 @@ def scan_forward(x, dt, A, Bm, Cm, D=None, dt_bias=None, *, softplus=True, h_in=
     args, (T, B, F, G, S), cfg = _scan_args(x, dt, A, Bm, Cm, D, dt_bias, softplus, h_in, lengths)
     x = args[0]
     _dense("h_out", h_out, x, (B, F, S))
-    if train and h_out is not None and h_out is h_in:
+    if train and h_out is not None and h_in is not None and h_out.data_ptr() == h_in.data_ptr() and h_in.numel():
         raise ValueError("the backward reads h_in: h_out must be another tensor")
     y = torch.empty_like(x)
     saved = x.new_empty(native.snn_scan_saved_bytes(cfg, T, B, F), dtype=torch.uint8) if train else None

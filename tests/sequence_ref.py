@@ -108,12 +108,12 @@ def scan(x, dt, A, Bm, Cm, D=None, dt_bias=None, *, softplus=True, h_in=None, le
     per = F // G
     Bf, Cf = (torch.where(m[..., None], t.repeat_interleave(per, 2), zero) for t in (Ba, Ca))
     h = torch.zeros(B, F, S, dtype=F64) if ha is None else ha
-    Dv = torch.zeros(F, dtype=F64) if Da is None else Da
+    through_d = lambda v: 0.0 if Da is None else Da * v  # noqa: E731
     hs, decays = [h], []
     for t in range(T):
         decays.append(torch.exp(d[t][..., None] * At))
         hs.append(decays[t] * hs[-1] + (dm[t] * xa[t])[..., None] * Bf[t])
-    y = torch.stack([(hs[t + 1] * Cf[t]).sum(-1) + Dv * xa[t] for t in range(T)]) if T else xa
+    y = torch.stack([(hs[t + 1] * Cf[t]).sum(-1) + through_d(xa[t]) for t in range(T)]) if T else xa
     out = {"y": torch.where(m, y, zero), "h_out": hs[-1]}
     if gy is None:
         return out
@@ -128,7 +128,7 @@ def scan(x, dt, A, Bm, Cm, D=None, dt_bias=None, *, softplus=True, h_in=None, le
         gCf[t] = gya[t][..., None] * hs[t + 1]
         gBf[t] = dh * (dm[t] * xa[t])[..., None]
         through = (dh * Bf[t]).sum(-1)
-        g["gx"][t] = dm[t] * through + Dv * gya[t]
+        g["gx"][t] = dm[t] * through + through_d(gya[t])
         gd = (q * rate).sum(-1) + xa[t] * through
         g["gdt"][t] = gd * (torch.sigmoid(v[t]) if softplus else 1.0)
         g["gA"] += (q * dm[t][..., None]).sum(0)
