@@ -9,7 +9,7 @@
 namespace snnlif {
 
 constexpr int64_t kMaxSeqT = int64_t(1) << 30, kMaxSeqB = int64_t(1) << 24, kMaxSeqF = int64_t(1) << 24;
-constexpr int64_t kMaxRows = int64_t(1) << 31, kMaxSpan = int64_t(1) << 44;
+constexpr int64_t kMaxRows = int64_t(1) << 30, kMaxSpan = int64_t(1) << 44;
 constexpr int kMaxTaps = 8, kMaxStates = 64;
 
 inline snn_status check_io(int io) { return io == SNN_IO_F32 || io == SNN_IO_BF16 ? SNN_OK : SNN_E_PARAM; }

@@ -87,8 +87,13 @@ struct Columns {
     unsigned lane;   // bytes
     __device__ Columns(const Rows& r, const ScanPlace& s)
         : base(static_cast<const char*>(r.p) + s.b * r.b * kBytes), step(r.t * kBytes), lane(unsigned(s.f) * kBytes) {}
-    __device__ auto load(int t) const { return IoVec<IO, 1>::load(base + t * step + lane, 0); }
-    __device__ void store(int t, float v) const { store1<IO>(const_cast<char*>(base + t * step + lane), v); }
+    __device__ const char* row(int t) const {
+        int64_t at = t * step;
+        asm("" : "+s"(at));      // or the product moves to the vector ALU, as one with the lane's offset
+        return base + at;
+    }
+    __device__ auto load(int t) const { return IoVec<IO, 1>::load(row(t) + lane, 0); }
+    __device__ void store(int t, float v) const { store1<IO>(const_cast<char*>(row(t) + lane), v); }
 };
 
 // B and C of one step and group are the same for every lane of a wave.  Each block of steps is

@@ -45,7 +45,7 @@ snn_status check_scan(const snn_scan_cfg* c, int64_t T, int64_t B, int64_t F) {
 snn_status check_norm(const snn_norm_cfg* c, int64_t T, int64_t B, int64_t F) {
     const snn_status st = check_norm_cfg(c);
     if (st != SNN_OK) return st;
-    if (check_seq_shape(T, B, F) != SNN_OK || T * B > kMaxBlocks) return SNN_E_SHAPE;
+    if (check_seq_shape(T, B, F) != SNN_OK) return SNN_E_SHAPE;
     return SNN_OK;
 }
 
