@@ -67,6 +67,31 @@ __host__ __device__ bool conv_state_later(const ConvArgs& a) {
     return a.plan.chunks > 1 && a.state_out == a.state_in;
 }
 
+// A lane's column of a [T][B][F] tensor, V features wide.
+template <int IO, int V>
+struct WideColumn {
+    static constexpr int kBytes = IO == SNN_IO_F32 ? 4 : 2;
+    char* p;         // row 0
+    int64_t step;    // bytes
+    __device__ WideColumn(const Rows& r, const ConvLane& l)
+        : p(static_cast<char*>(at_out<IO>(r, 0, l.b, l.f))), step(r.t * kBytes) {}
+    __device__ auto load(int64_t t) const { return IoVec<IO, V>::load(p + t * step, 0); }
+    __device__ void store(int64_t t, const float (&v)[V]) const { IoVec<IO, V>::store(p + t * step, 0, v); }
+};
+
+// Rows t .. t+U-1 below `stop`, without a branch per row where all of them are.
+template <int U, typename Col, typename Raw>
+__device__ __forceinline__ void load_rows_ahead(const Col& c, int64_t t, int64_t stop, Raw (&raw)[U]) {
+    if (t + U <= stop) {
+#pragma unroll
+        for (int k = 0; k < U; ++k) raw[k] = c.load(t + k);
+    } else {
+#pragma unroll
+        for (int k = 0; k < U; ++k)
+            if (t + k < stop) raw[k] = c.load(t + k);
+    }
+}
+
 template <int IO, int W, int ACT, int V>
 __device__ void conv_forward_walk(const ConvArgs& a, const ConvLane& l) {
     constexpr int U = conv_rows(false);     // rows in flight
@@ -74,37 +99,38 @@ __device__ void conv_forward_walk(const ConvArgs& a, const ConvLane& l) {
     load_filter<W, V>(a, l.f, w, bias);
     const int64_t len = steps_of(a.lengths, l.b, a.T), t0 = l.c * a.plan.steps;
     const int64_t end = min(a.T, t0 + a.plan.steps), stop = min(end, len);
+    const WideColumn<IO, V> cx(a.x, l), cy(a.y, l);
     if (t0 < stop) {
 #pragma unroll
         for (int i = 0; i < W - 1; ++i) conv_input<IO, W, V>(a, t0 - (W - 1) + i, l.b, l.f, hist[i]);
     }
     typename IoVec<IO, V>::raw raw[U], ahead[U];
-    const auto fetch = [&](int64_t t) {
+    const auto row = [&](int64_t t, const typename IoVec<IO, V>::raw& x) {
+        float u[V];
 #pragma unroll
-        for (int k = 0; k < U; ++k)
-            if (t + k < stop) ahead[k] = IoVec<IO, V>::load(at<IO>(a.x, t + k, l.b, l.f), 0);
+        for (int j = 0; j < V; ++j) {
+            hist[W - 1][j] = IoVec<IO, V>::get(x, j);
+            u[j] = bias[j];
+#pragma unroll
+            for (int i = 0; i < W; ++i) u[j] = fmaf(w[j][i], hist[i][j], u[j]);
+#pragma unroll
+            for (int i = 0; i < W - 1; ++i) hist[i][j] = hist[i + 1][j];
+            if (ACT == SNN_ACT_SILU) u[j] *= sigmoid(u[j]);
+        }
+        cy.store(t, u);
     };
-    fetch(t0);
+    load_rows_ahead<U>(cx, t0, stop, ahead);
     for (int64_t t = t0; t < stop; t += U) {
 #pragma unroll
         for (int k = 0; k < U; ++k) raw[k] = ahead[k];
-        fetch(t + U);
+        load_rows_ahead<U>(cx, t + U, stop, ahead);
+        if (t + U <= stop) {
 #pragma unroll
-        for (int k = 0; k < U; ++k) {
-            if (t + k < stop) {
-                float u[V];
+            for (int k = 0; k < U; ++k) row(t + k, raw[k]);
+        } else {
 #pragma unroll
-                for (int j = 0; j < V; ++j) {
-                    hist[W - 1][j] = IoVec<IO, V>::get(raw[k], j);
-                    u[j] = bias[j];
-#pragma unroll
-                    for (int i = 0; i < W; ++i) u[j] = fmaf(w[j][i], hist[i][j], u[j]);
-#pragma unroll
-                    for (int i = 0; i < W - 1; ++i) hist[i][j] = hist[i + 1][j];
-                    if (ACT == SNN_ACT_SILU) u[j] *= sigmoid(u[j]);
-                }
-                IoVec<IO, V>::store(at_out<IO>(a.y, t + k, l.b, l.f), 0, u);
-            }
+            for (int k = 0; k < U; ++k)
+                if (t + k < stop) row(t + k, raw[k]);
         }
     }
     float zero[V] = {};
@@ -152,14 +178,17 @@ __device__ void conv_backward_walk(const ConvArgs& a, const ConvLane& l) {
         for (int i = 0; i < W; ++i) gw[j][i] = gu[i][j] = 0.0f;
     }
     // dL/dx[s] from gu[i] = dL/du[s + i], and the state's gradient where input s is part of it
-    const auto emit = [&](int64_t s) {
-        float g[V];
+    const auto grad_x = [&](float (&g)[V]) {
 #pragma unroll
         for (int j = 0; j < V; ++j) {
             g[j] = 0.0f;
 #pragma unroll
             for (int i = 0; i < W; ++i) g[j] = fmaf(w[j][W - 1 - i], gu[i][j], g[j]);
         }
+    };
+    const auto emit = [&](int64_t s) {
+        float g[V];
+        grad_x(g);
         const int64_t i = s - (len - (W - 1));
         if (a.gstate_out != nullptr && i >= 0 && i < W - 1) {
             float e[V];
@@ -183,46 +212,53 @@ __device__ void conv_backward_walk(const ConvArgs& a, const ConvLane& l) {
 #pragma unroll
         for (int i = 0; i < W - 1; ++i) conv_input<IO, W, V>(a, t0 - (W - 1) + i, l.b, l.f, hist[i]);
         typename IoVec<IO, V>::raw xr[U], gr[U], xa[U], ga[U];
-        const auto fetch = [&](int64_t t) {
+        const WideColumn<IO, V> cx(a.x, l), cgy(a.gy, l), cgx(a.gx, l);
+        // inner rows: every step of the batch is the chunk's own, and so is the input W-1 steps
+        // before, which is part of no state
+        const auto row = [&](auto inner, int64_t t, const typename IoVec<IO, V>::raw& x, const typename IoVec<IO, V>::raw& gy) {
+            float g[V];
 #pragma unroll
-            for (int k = 0; k < U; ++k) {
-                if (t + k < past) {
-                    xa[k] = IoVec<IO, V>::load(at<IO>(a.x, t + k, l.b, l.f), 0);
-                    ga[k] = IoVec<IO, V>::load(at<IO>(a.gy, t + k, l.b, l.f), 0);
-                }
+            for (int j = 0; j < V; ++j) {
+                hist[W - 1][j] = IoVec<IO, V>::get(x, j);
+                float u = bias[j];
+#pragma unroll
+                for (int i = 0; i < W; ++i) u = fmaf(w[j][i], hist[i][j], u);
+                g[j] = IoVec<IO, V>::get(gy, j);
+                if (ACT == SNN_ACT_SILU) g[j] *= silu_slope(u, sigmoid(u));
+                const float own = inner.value || t < stop ? g[j] : 0.0f;   // steps past the chunk are another's
+                gb[j] += own;
+#pragma unroll
+                for (int i = 0; i < W; ++i) gw[j][i] = fmaf(own, hist[i][j], gw[j][i]);
+#pragma unroll
+                for (int i = 0; i < W - 1; ++i) hist[i][j] = hist[i + 1][j];
+            }
+            push(g);
+            const int64_t s = t - (W - 1);
+            if constexpr (inner.value) {
+                float gx[V];
+                grad_x(gx);
+                cgx.store(s, gx);
+            } else {
+                if (s >= t0 || t0 == 0) emit(s);
             }
         };
-        fetch(t0);
+        load_rows_ahead<U>(cx, t0, past, xa);
+        load_rows_ahead<U>(cgy, t0, past, ga);
         for (int64_t t = t0; t < past; t += U) {
 #pragma unroll
             for (int k = 0; k < U; ++k) {
                 xr[k] = xa[k];
                 gr[k] = ga[k];
             }
-            fetch(t + U);
+            load_rows_ahead<U>(cx, t + U, past, xa);
+            load_rows_ahead<U>(cgy, t + U, past, ga);
+            if (t >= t0 + (W - 1) && t + U <= stop) {
 #pragma unroll
-            for (int k = 0; k < U; ++k) {
-                if (t + k < past) {
-                    float g[V];
+                for (int k = 0; k < U; ++k) row(std::true_type{}, t + k, xr[k], gr[k]);
+            } else {
 #pragma unroll
-                    for (int j = 0; j < V; ++j) {
-                        hist[W - 1][j] = IoVec<IO, V>::get(xr[k], j);
-                        float u = bias[j];
-#pragma unroll
-                        for (int i = 0; i < W; ++i) u = fmaf(w[j][i], hist[i][j], u);
-                        g[j] = IoVec<IO, V>::get(gr[k], j);
-                        if (ACT == SNN_ACT_SILU) g[j] *= silu_slope(u, sigmoid(u));
-                        const float own = t + k < stop ? g[j] : 0.0f;   // steps past the chunk are another's
-                        gb[j] += own;
-#pragma unroll
-                        for (int i = 0; i < W; ++i) gw[j][i] = fmaf(own, hist[i][j], gw[j][i]);
-#pragma unroll
-                        for (int i = 0; i < W - 1; ++i) hist[i][j] = hist[i + 1][j];
-                    }
-                    push(g);
-                    const int64_t s = t + k - (W - 1);
-                    if (s >= t0 || t0 == 0) emit(s);
-                }
+                for (int k = 0; k < U; ++k)
+                    if (t + k < past) row(std::false_type{}, t + k, xr[k], gr[k]);
             }
         }
         // the steps after the sequence's last have no gradient
