@@ -14,6 +14,7 @@ from concurrent.futures import ThreadPoolExecutor
 HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
+CSRC_SEQ = os.path.join(HERE, "csrc_seq")   # the sequence operators (include/snn_seq.h)
 OUT = os.path.join(HERE, "libsnnlif.so")
 OBJ_DIR = os.path.join(HERE, "_build")
 
@@ -38,15 +39,15 @@ UNITS = (
        for io in (0, 1) for spk in (0, 1, 2)]
     + [(f"stackb_io{io}", "lif_stack.hip", [f"-DSNNLIF_IO={io}", "-DSNNLIF_STACK_BWD=1"]) for io in (0, 1)]
     + [("glue", "lif_glue.hip", []), ("serial", "lif_serial.hip", []), ("api", "snn_lif_api.hip", [])]
-    + [(name, f"{name}.hip", []) for name in ("seq_conv", "seq_scan_forward", "seq_scan_backward", "seq_scan_split",
-                                              "seq_norm", "snn_seq_api")]
+    + [(name, os.path.join(CSRC_SEQ, f"{name}.hip"), [])
+       for name in ("seq_conv", "seq_scan_forward", "seq_scan_backward", "seq_scan_split", "seq_norm", "snn_seq_api")]
 )
 
 
 def _compile(unit, extra):
     name, src, defs = unit
     obj = os.path.join(OBJ_DIR, name + ".o")
-    cmd = ["hipcc", *HIPCC_FLAGS, *extra, *defs, "-I", os.path.join(ROOT, "include"), "-I", CSRC,
+    cmd = ["hipcc", *HIPCC_FLAGS, *extra, *defs, "-I", os.path.join(ROOT, "include"), "-I", CSRC, "-I", CSRC_SEQ,
            "-c", os.path.join(CSRC, src), "-o", obj]
     r = subprocess.run(cmd, capture_output=True, text=True)
     noise = "'-packed-fp32-ops' is not a recognized feature for this target (ignoring feature)"

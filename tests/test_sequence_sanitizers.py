@@ -1,5 +1,5 @@
 """AddressSanitizer and UndefinedBehaviorSanitizer over the sequence operators' host code, on the
-CPU: argument checks and plans (csrc/seq_host.h, compiled by g++ as host code only), driven by
+CPU: argument checks and plans (csrc_seq/seq_host.h, compiled by g++ as host code only), driven by
 tests/sanitize/seq_harness.cpp.  No GPU code is built here."""
 import os
 import shutil
@@ -17,7 +17,7 @@ def test_host_code_under_sanitizers(tmp_path):
     exe = tmp_path / "seq_harness"
     subprocess.run(["g++", "-std=c++17", *SAN, "-D__HIP_PLATFORM_AMD__", "-I", os.path.join(rocm, "include"),
                     "-I", os.path.join(ROOT, "include"), "-I", os.path.join(ROOT, "paper_2408_00280_amd", "csrc"),
-                    os.path.join(ROOT, "tests", "sanitize", "seq_harness.cpp"), "-o", str(exe)], check=True)
+                    "-I", os.path.join(ROOT, "paper_2408_00280_amd", "csrc_seq"), os.path.join(ROOT, "tests", "sanitize", "seq_harness.cpp"), "-o", str(exe)], check=True)
     env = dict(os.environ, ASAN_OPTIONS="detect_leaks=1:halt_on_error=1:abort_on_error=0",
                UBSAN_OPTIONS="halt_on_error=1:print_stacktrace=1")
     r = subprocess.run([str(exe)], env=env, capture_output=True, text=True, timeout=300)
