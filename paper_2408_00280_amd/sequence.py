@@ -28,19 +28,22 @@ _conv_cfg, _scan_cfg, _norm_cfg = (functools.lru_cache(maxsize=64)(c) for c in (
 
 def _on_stream(fn):
     """fn with its first tensor's device as the current one, on `stream`."""
+    first = fn.__code__.co_varnames[0]
+
     @functools.wraps(fn)
-    def call(x, *args, stream=None, **kw):
+    def call(*args, stream=None, **kw):
+        x = args[0] if args else kw[first]
         if not x.is_cuda:
             raise ValueError("tensors must be on the GPU")
-        if stream is None and x.device.index == torch._C._cuda_getDevice():
-            return fn(x, *args, **kw)
+        if stream is None and x.get_device() == torch._C._cuda_getDevice():
+            return fn(*args, **kw)
         with torch.cuda.device(x.device):
             if stream is None:
-                return fn(x, *args, **kw)
+                return fn(*args, **kw)
             if not isinstance(stream, torch.cuda.Stream):
                 stream = torch.cuda.ExternalStream(int(stream)) if stream else torch.cuda.default_stream()
             with torch.cuda.stream(stream):
-                return fn(x, *args, **kw)
+                return fn(*args, **kw)
     return call
 
 

@@ -292,7 +292,7 @@ def test_norm(ops, io, T, B, F, parts, ragged, layout, given):
                 assert not g.any()
             else:
                 R.check(name, g, ref[name], mag[name], n)
-    again = ops.norm_forward(*args, lengths=ln)
+    again = ops.norm_forward(y=args[0], **dict(zip(("r", "z", "w_post", "scale", "w_pre"), args[1:])), lengths=ln)
     assert torch.equal(again[0], r_new) and again[2] is None
 
 
