@@ -139,4 +139,14 @@ struct BCColumns {
     }
 };
 
+// Values loaded before a loop have come when it starts.  Left pending they are waited for at
+// their use inside, in every round, and with them the loads and stores that the loop itself
+// has under way by then.
+__device__ __forceinline__ void settle(float& v) { asm volatile("" : "+v"(v)); }
+template <int N>
+__device__ __forceinline__ void settle(float (&v)[N]) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) settle(v[i]);
+}
+
 }  // namespace snnlif

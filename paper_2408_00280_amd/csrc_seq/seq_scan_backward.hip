@@ -38,14 +38,15 @@ __device__ __forceinline__ float reduce8(const float (&v)[8], int lane) {
     return r;
 }
 
-struct Step {
-    float d, dx, gy;    // d, d x, dL/dy
+struct __align__(16) Step {
+    float d, dx, gy, x;    // d, d x, dL/dy, x
 };
 
 template <int NS>
 struct BackwardLds {
     static constexpr int K = scan_keep(NS);
     Step sd[2][K][kWave];        // this block's, and the next one's as it is staged
+    float slope[2][K][kWave];    // of the softplus
     StagedBC<NS, K> sbc[2];
     float2 sg[NS][K][kWave];     // (sum dh B, sum dh a h A log2 e)
     float sgbc[K][NS][2 * kSL];  // dL/dB and dL/dC
@@ -72,7 +73,7 @@ __global__ __launch_bounds__(NS * kWave, NS > 8 ? 4 : 2) void scan_backward_kern
     load(a.gh_out, StateColumn(a, p, a.part_h), blockIdx.y, a.plan.segments == 1, e);
 #pragma unroll
     for (int i = 0; i < kSL; ++i) gA[i] = 0.0f;
-    const float skip = a.D != nullptr ? a.D[p.f] : 0.0f, bias = a.dt_bias != nullptr ? a.dt_bias[p.f] : 0.0f;
+    float skip = a.D != nullptr ? a.D[p.f] : 0.0f, bias = a.dt_bias != nullptr ? a.dt_bias[p.f] : 0.0f;
     const Columns<IO> cx(a.x, p), cdt(a.dt, p), cgy(a.gy, p), cgx(a.gx, p), cgdt(a.gdt, p);
     const bool busy = p.states > 0;
     const int used = (a.S + kSL - 1) / kSL;
@@ -81,7 +82,6 @@ __global__ __launch_bounds__(NS * kWave, NS > 8 ? 4 : 2) void scan_backward_kern
         typename IoVec<IO, 1>::raw x, dt, gy;
     };
     Raw raw[R];                  // of the next block
-    float own[R][2];             // x and the softplus' slope of this block, for its end
     const auto fetch_rows = [&](int t0) {
 #pragma unroll
         for (int r = 0; r < R; ++r) {
@@ -89,19 +89,21 @@ __global__ __launch_bounds__(NS * kWave, NS > 8 ? 4 : 2) void scan_backward_kern
             if (k < K && t0 >= p.t0 && t0 + k < p.len) raw[r] = {cx.load(t0 + k), cdt.load(t0 + k), cgy.load(t0 + k)};
         }
     };
-    const auto stage_rows = [&](int t0, int to, float (&mine)[R][2]) {
+    const auto stage_rows = [&](int t0, int to) {
 #pragma unroll
         for (int r = 0; r < R; ++r) {
             const int k = p.wave + r * NS;
-            Step d = {0.0f, 0.0f, 0.0f};
+            Step d = {0.0f, 0.0f, 0.0f, 0.0f};
+            float slope = 1.0f;
             if (k < K && t0 >= p.t0 && t0 + k < p.len) {
                 const float v = IoVec<IO, 1>::get(raw[r].dt, 0) + bias, x = IoVec<IO, 1>::get(raw[r].x, 0);
-                mine[r][0] = x;
-                mine[r][1] = 1.0f;
-                const float step = a.softplus ? softplus(v, mine[r][1]) : v;
-                if (p.active) d = {step, step * x, IoVec<IO, 1>::get(raw[r].gy, 0)};
+                const float step = a.softplus ? softplus(v, slope) : v;
+                if (p.active) d = {step, step * x, IoVec<IO, 1>::get(raw[r].gy, 0), x};
             }
-            if (k < K) m.sd[to][k][p.lane] = d;
+            if (k < K) {
+                m.sd[to][k][p.lane] = d;
+                m.slope[to][k][p.lane] = slope;
+            }
         }
     };
     const StateColumn kept(a, p, a.saved);
@@ -120,12 +122,12 @@ __global__ __launch_bounds__(NS * kWave, NS > 8 ? 4 : 2) void scan_backward_kern
         cbc.template fetch<-1>(t0, p.t0, p.len);
         fetch_rows(t0);
     };
-    const auto stage = [&](int t0, int to, float (&mine)[R][2]) {
+    const auto stage = [&](int t0, int to) {
         if (t0 >= p.t0) cbc.stage(t0, p.len, m.sbc[to]);
-        stage_rows(t0, to, mine);
+        stage_rows(t0, to);
     };
     fetch(t0);
-    stage(t0, 0, own);
+    stage(t0, 0);
     fetch(t0 - K);
     float h[kSL], h_next[kSL];
     struct Ahead {
@@ -137,6 +139,11 @@ __global__ __launch_bounds__(NS * kWave, NS > 8 ? 4 : 2) void scan_backward_kern
         return Ahead{m.sd[block][k][p.lane], bc[0], bc[1]};
     };
     load(a.h_in, kept, t0 / K - 1, t0 <= 0, h);
+    settle(skip);
+    settle(bias);
+    settle(rate);
+    settle(e);
+    settle(h);
     lds_barrier();
     int buf = 0;
     for (; t0 >= p.t0; t0 -= K) {
@@ -192,11 +199,11 @@ __global__ __launch_bounds__(NS * kWave, NS > 8 ? 4 : 2) void scan_backward_kern
                 if (kAhead) step = ahead;
             }
             sum_up(0);
+            settle(h_next);      // half a block after their load, and not with the next block's loads
 #pragma unroll
             for (int s = 0; s < kSL; ++s) h[s] = h_next[s];
         }
-        float staged[R][2];
-        stage(t0 - K, buf ^ 1, staged);
+        stage(t0 - K, buf ^ 1);
         fetch(t0 - 2 * K);
         lds_barrier();
 #pragma unroll
@@ -216,9 +223,8 @@ __global__ __launch_bounds__(NS * kWave, NS > 8 ? 4 : 2) void scan_backward_kern
                         da += w < used ? g[w].y : 0.0f;
                     }
                     gx = fmaf(s.d, db, a.D != nullptr ? skip * s.gy : 0.0f);
-                    const float x = own[r][0];
-                    gdt = fmaf(x, db, da * kLn2) * own[r][1];    // rate is A log2 e
-                    gD = fmaf(s.gy, x, gD);
+                    gdt = fmaf(s.x, db, da * kLn2) * m.slope[buf][k][p.lane];   // rate is A log2 e
+                    gD = fmaf(s.gy, s.x, gD);
                     gbias += gdt;
                 }
                 if (p.active) {
@@ -226,8 +232,6 @@ __global__ __launch_bounds__(NS * kWave, NS > 8 ? 4 : 2) void scan_backward_kern
                     cgdt.store(t0 + k, gdt);
                 }
             }
-            own[r][0] = staged[r][0];
-            own[r][1] = staged[r][1];
         }
         {
             const int64_t row = int64_t(a.B) * a.G * (NS * 2 * kSL);

@@ -6,8 +6,8 @@
 // vector ALU.  A lane is a feature and each wave of a workgroup holds 4 of its states in
 // registers.  What belongs to a step but not to a state (the softplus, B and C, the sum of y
 // over the waves) is shared out over the waves, K steps at a time, through LDS: while a
-// block's steps run, the one after the next is staged and the third is loaded, and one
-// barrier parts two blocks.
+// block's steps run, the one after the next is loaded, and staged before the barrier that
+// parts two blocks.
 #include "seq_scan.h"
 
 namespace snnlif {
@@ -24,7 +24,11 @@ __global__ __launch_bounds__(NS * kWave) void scan_forward_kernel(ScanArgs a) {
     load_rates(a, p, rate);
     if (a.plan.segments == 1) load_state(a, p, a.h_in, h);
     else if (p.states > 0) StateColumn(a, p, a.part_h).load(blockIdx.y, h);
-    const float skip = a.D != nullptr ? a.D[p.f] : 0.0f, bias = a.dt_bias != nullptr ? a.dt_bias[p.f] : 0.0f;
+    float skip = a.D != nullptr ? a.D[p.f] : 0.0f, bias = a.dt_bias != nullptr ? a.dt_bias[p.f] : 0.0f;
+    settle(skip);
+    settle(bias);
+    settle(rate);
+    settle(h);
     const Columns<IO> cx(a.x, p), cdt(a.dt, p), cy(a.y, p);
     BCColumns<IO, NS, K> cbc(a, p, p.t0);
     const StateColumn kept(a, p, a.saved);
@@ -65,7 +69,6 @@ __global__ __launch_bounds__(NS * kWave) void scan_forward_kernel(ScanArgs a) {
     stage(p.t0, 0, xs[0]);
     fetch(p.t0 + K);
     stage(p.t0 + K, 1, xs[1]);
-    fetch(p.t0 + 2 * K);
     struct Step {
         float2 d;
         f32x4_t b, c;
@@ -83,8 +86,7 @@ __global__ __launch_bounds__(NS * kWave) void scan_forward_kernel(ScanArgs a) {
         if (t0 < p.len) {
             if (a.saved != nullptr && t0 > 0 && (t0 & (a.plan.keep - 1)) == 0)
                 if (busy && p.active) kept.store(t0 / a.plan.keep - 1, h);
-            stage(t0 + 2 * K, last, xs[2]);
-            fetch(t0 + 3 * K);
+            fetch(t0 + 2 * K);
             if (busy) {
 #pragma unroll
                 for (int u = 0; u < K; u += U) {
@@ -107,6 +109,8 @@ __global__ __launch_bounds__(NS * kWave) void scan_forward_kernel(ScanArgs a) {
                     for (int i = 0; i < U; ++i) step[i] = ahead[i];
                 }
             }
+            // here, a block's steps after the last stores and the loads, neither is waited for long
+            stage(t0 + 2 * K, last, xs[2]);
         }
         lds_barrier();
 #pragma unroll
@@ -144,7 +148,11 @@ __global__ __launch_bounds__(kWave) void scan_forward_one_kernel(ScanArgs a) {
     load_rates(a, p, rate);
     if (a.plan.segments == 1) load_state(a, p, a.h_in, h);
     else StateColumn(a, p, a.part_h).load(blockIdx.y, h);
-    const float skip = a.D != nullptr ? a.D[p.f] : 0.0f, bias = a.dt_bias != nullptr ? a.dt_bias[p.f] : 0.0f;
+    float skip = a.D != nullptr ? a.D[p.f] : 0.0f, bias = a.dt_bias != nullptr ? a.dt_bias[p.f] : 0.0f;
+    settle(skip);
+    settle(bias);
+    settle(rate);
+    settle(h);
     const Columns<IO> cx(a.x, p), cdt(a.dt, p), cy(a.y, p);
     const StateColumn kept(a, p, a.saved);
     BCColumns<IO, 1, K> cbc(a, p, p.t0);
@@ -161,6 +169,12 @@ __global__ __launch_bounds__(kWave) void scan_forward_one_kernel(ScanArgs a) {
     };
     fetch(p.t0);
     int buf = 0;
+    float ys[K];     // of the block before: stored once this block's loads have come, not waited for with them
+    const auto put = [&](int t0) {
+#pragma unroll
+        for (int k = 0; k < K; ++k)
+            if (t0 + k < p.len && p.active) cy.store(t0 + k, ys[k]);
+    };
     for (int t0 = p.t0; t0 < p.t1; t0 += K, buf ^= 1) {
         const int n = min(K, p.len - t0);                        // steps inside the sequence
         if (n > 0) {
@@ -177,6 +191,7 @@ __global__ __launch_bounds__(kWave) void scan_forward_one_kernel(ScanArgs a) {
                 }
             }
             cbc.stage(t0, p.len, sbc[buf]);
+            if (t0 > p.t0) put(t0 - K);
             fetch(t0 + K);
             lds_barrier();
             const f32x4_t* bc = reinterpret_cast<const f32x4_t*>(sbc[buf].v[0][0]);
@@ -189,8 +204,9 @@ __global__ __launch_bounds__(kWave) void scan_forward_one_kernel(ScanArgs a) {
                     h[s] = fmaf(__builtin_amdgcn_exp2f(d[k] * rate[s]), h[s], (d[k] * x[k]) * b[s]);
                     y = FULL || s < p.states ? fmaf(c[s], h[s], y) : y;
                 }
-                if (k < n && p.active) cy.store(t0 + k, y);
+                ys[k] = y;
             }
+            if (t0 + K >= min(p.t1, p.len)) put(t0);             // the last block
         }
         for (int k = max(n, 0); k < K && t0 + k < p.t1; ++k)
             if (p.active) cy.store(t0 + k, 0.0f);

@@ -21,7 +21,7 @@ __global__ __launch_bounds__(NS * kWave) void scan_local_kernel(ScanArgs a) {
     __shared__ __align__(16) StagedBC<NS, K> sbc[3];
     // the first segment's state is not needed further down, nor the last one's further up
     const ScanPlace p = scan_place(a, DOWN ? 1 : 0);
-    const float bias = a.dt_bias != nullptr ? a.dt_bias[p.f] : 0.0f;
+    float bias = a.dt_bias != nullptr ? a.dt_bias[p.f] : 0.0f;
     const Columns<IO> cv(DOWN ? a.gy : a.x, p), cdt(a.dt, p);
     const StateColumn out(a, p, a.part_h);
     const bool busy = p.states > 0;
@@ -30,6 +30,8 @@ __global__ __launch_bounds__(NS * kWave) void scan_local_kernel(ScanArgs a) {
     BCColumns<IO, NS, K> cbc(a, p, start(0));
     float rate[kSL], h[kSL], sum = 0.0f;
     load_rates(a, p, rate);
+    settle(bias);
+    settle(rate);
 #pragma unroll
     for (int s = 0; s < kSL; ++s) h[s] = 0.0f;
 
