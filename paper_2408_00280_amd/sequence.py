@@ -82,9 +82,9 @@ def _bytes(n, x):
     return x.new_empty(n, dtype=torch.uint8) if n else None
 
 
-def _params(shape, x, empty):
+def _params(p, empty):
     """A parameter's gradient: the kernels write it whole, unless there is nothing to do."""
-    return (torch.zeros if empty else torch.empty)(shape, dtype=torch.float32, device=x.device)
+    return None if p is None else (torch.zeros_like if empty else torch.empty_like)(p)
 
 
 def _hand_over(out, given):
@@ -131,8 +131,7 @@ def conv_backward(x, weight, bias, grad_y, *, act="silu", state=None, lengths=No
     gy = _data("grad_y", grad_y, x, (T, B, F))
     _dense("grad_state_out", grad_state_out, x, (W - 1, B, F), x.dtype)
     empty = not x.numel()
-    gx, gw = torch.empty_like(x), _params((F, W), x, empty)
-    gb = None if bias is None else _params((F,), x, empty)
+    gx, gw, gb = torch.empty_like(x), _params(weight, empty), _params(bias, empty)
     gs = None if state is None else torch.empty_like(state)
     if empty:
         _hand_over(gs, grad_state_out)
@@ -196,9 +195,7 @@ def scan_backward(x, dt, A, Bm, Cm, D, dt_bias, saved, grad_y, *, softplus=True,
     _dense("grad_h_out", grad_h_out, x, (B, F, S))
     empty = not x.numel()
     gx, gdt, gB, gC = torch.empty_like(x), torch.empty_like(x), torch.empty_like(args[3]), torch.empty_like(args[4])
-    gA = _params((F, S), x, empty)
-    gD = None if D is None else _params((F,), x, empty)
-    gbias = None if dt_bias is None else _params((F,), x, empty)
+    gA, gD, gbias = _params(A, empty), _params(D, empty), _params(dt_bias, empty)
     gh = None if h_in is None else torch.empty_like(h_in)
     if empty:
         gB.zero_(), gC.zero_()
@@ -248,7 +245,7 @@ def norm_backward(y, r, z, w_post, scale, w_pre, rstd, grad_r_new, grad_u=None, 
     g2 = None if grad_u is None else _data("grad_u", grad_u, y, (T, B, F))
     empty = not y.numel()
     gy, gr, gz = (None if a is None else torch.empty_like(a) for a in (args[0], args[2], args[1]))
-    gw = [None if w is None else _params((F,), y, empty) for w in (w_post, scale, w_pre)]
+    gw = [_params(w, empty) for w in (w_post, scale, w_pre)]
     if not empty:
         ws = _bytes(native.snn_norm_workspace_bytes(cfg, T, B, F), y)
         native.snn_norm_backward(cfg, T, B, F, *args, rstd, g1, g2, gy, gz, gr, *gw, ws)
