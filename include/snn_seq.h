@@ -18,8 +18,8 @@
  *     steps.  Rows behind them are padding: inputs there are not read (whatever they hold),
  *     outputs and gradients there are written as 0, states stay as they were at the end.
  *   - T == 0, B == 0 or F == 0 is an empty problem: SNN_OK, nothing is launched or written.
- *   - Limits: T <= 2^30, B <= 2^24, F <= 2^24, T * B <= 2^30, B * F <= 2^31 in
- *     the scan, and every tensor spans less than 2^44 elements.
+ *   - Limits: T <= 2^30, B <= 2^24, F <= 2^24, T * B <= 2^30, B * F <= 2^31 and
+ *     T * B * groups < 2^31 in the scan, and every tensor spans less than 2^44 elements.
  *   - A workspace is scratch: it holds nothing between calls, and calls that may run at the
  *     same time need one each.
  * Results do not change from run to run: sums over steps, sequences and features are formed

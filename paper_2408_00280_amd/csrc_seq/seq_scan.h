@@ -39,10 +39,17 @@ __device__ __forceinline__ ScanPlace scan_place(const ScanArgs& a, int first_seg
 // Where S is not whole lanes (FULL = false in the kernels), the last wave leaves its states
 // behind the last one out of its sums: B = C = 0 there, which gives 0 with finite values only.
 
-// A[f][n] log2(e) of the lane's states, 0 behind the last.
+// A log2(e), kept finite: steps behind a sequence's end have d = 0 and are to leave the state as
+// it is, which 2^(0 A) does not where A is infinite or becomes so with the factor.
+__device__ __forceinline__ float rate_of(float A) {
+    const float r = A * kLog2e;
+    return fabsf(r) == __builtin_inff() ? copysignf(__FLT_MAX__, r) : r;
+}
+
+// The rates of the lane's states, 0 behind the last.
 __device__ __forceinline__ void load_rates(const ScanArgs& a, const ScanPlace& p, float (&r)[kSL]) {
 #pragma unroll
-    for (int i = 0; i < kSL; ++i) r[i] = i < p.states ? a.A[p.f * a.S + p.first + i] * kLog2e : 0.0f;
+    for (int i = 0; i < kSL; ++i) r[i] = i < p.states ? rate_of(a.A[p.f * a.S + p.first + i]) : 0.0f;
 }
 
 __device__ __forceinline__ void load_state(const ScanArgs& a, const ScanPlace& p, const float* from, float (&h)[kSL]) {

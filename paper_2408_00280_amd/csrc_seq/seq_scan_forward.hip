@@ -273,7 +273,7 @@ __global__ __launch_bounds__(kBlock) void scan_token_kernel(ScanArgs a) {
             const float w = v[k] + bias, d = a.softplus ? softplus(w) : w;
 #pragma unroll
             for (int j = 0; j < kSL; ++j) {
-                h[k][j] = fmaf(__builtin_amdgcn_exp2f(d * (rate[j] * kLog2e)), h[k][j], (d * x[k]) * bv[k][j]);
+                h[k][j] = fmaf(__builtin_amdgcn_exp2f(d * rate_of(rate[j])), h[k][j], (d * x[k]) * bv[k][j]);
                 y = j < states ? fmaf(cv[k][j], h[k][j], y) : y;
             }
             y = q == 0 && a.D != nullptr ? fmaf(skip, x[k], y) : y;

@@ -130,7 +130,7 @@ __global__ __launch_bounds__(kBlock) void scan_carry_kernel(ScanArgs a, int64_t 
     if (i >= n) return;
     const int64_t states = n / (a.B * a.F), f = i % a.F, q = i / a.F, s = q % states, b = q / states;
     const bool in = s < a.S;
-    const float rate = in ? a.A[f * a.S + s] * kLog2e : 0.0f;
+    const float rate = in ? rate_of(a.A[f * a.S + s]) : 0.0f;
     const float* from = DOWN ? a.gh_out : a.h_in;
     float h = in && from != nullptr ? from[(b * a.F + f) * a.S + s] : 0.0f;
     constexpr int U = 4;

@@ -189,8 +189,9 @@ def scan_backward(x, dt, A, Bm, Cm, D, dt_bias, saved, grad_y, *, softplus=True,
     with the same arguments and what it saved; grad_h_out: the gradient of its h_out."""
     args, (T, B, F, G, S), cfg = _scan_args(x, dt, A, Bm, Cm, D, dt_bias, softplus, h_in, lengths)
     x = args[0]
-    if saved.dtype != torch.uint8 or saved.numel() != native.snn_scan_saved_bytes(cfg, T, B, F):
+    if saved is None:
         raise ValueError("saved must be what scan_forward(train=True) returned for these arguments")
+    _dense("saved", saved, x, (native.snn_scan_saved_bytes(cfg, T, B, F),), torch.uint8)
     gy = _data("grad_y", grad_y, x, (T, B, F))
     _dense("grad_h_out", grad_h_out, x, (B, F, S))
     empty = not x.numel()

@@ -239,6 +239,26 @@ def test_infinities_are_not_made_nan(ops, S, T):
         assert torch.equal(torch.isnan(v.cpu()), torch.isnan(ref[name])), name
 
 
+@pytest.mark.parametrize("S", [3, 16])
+@pytest.mark.parametrize("T", [1, 9, 150])
+def test_rates_whose_exponent_is_past_the_type(ops, T, S):
+    """A = -3e38 is finite and A log2(e) is not: such states forget all in a step, and keep
+    what they hold behind the end of their sequence."""
+    B, F = 3, 67
+    x, step, A, Bm, Cm, D, bias, h, gy, gh = scan_inputs("f32", T, B, F, S, 1, "D bias h")
+    A[::2, S - 1] = -3e38
+    ln = torch.tensor([T, T // 2, 0], dtype=torch.int32, device="cuda")
+    ref, mag = (R.scan(x, step, A, Bm, Cm, D, bias, h_in=h, lengths=ln.cpu(), gy=gy, gh_out=gh, mag=m) for m in (False, True))
+    out = torch.empty((B, F, S), device="cuda")
+    y, saved = ops.scan_forward(x, step, A, Bm, Cm, D, bias, h_in=h, h_out=out, lengths=ln, train=True)
+    got = ops.scan_backward(x, step, A, Bm, Cm, D, bias, saved, gy, h_in=h, lengths=ln, grad_h_out=gh)
+    n = R.scan_roundings(T, B, F, S)
+    for name, v in zip(("y", "h_out", *NAMES), (y, out, *got)):
+        R.check(name, v, ref[name], mag[name], n)
+    with pytest.raises(ValueError):
+        ops.scan_backward(x, step, A, Bm, Cm, D, bias, None, gy, h_in=h, lengths=ln, grad_h_out=gh)
+
+
 def test_block_captured_through_autograd(ops):
     """A block's forward and gradients captured into a graph with no eager graph of its leaves
     alive; every replay, with new inputs and other work in between, gives the eager values."""
