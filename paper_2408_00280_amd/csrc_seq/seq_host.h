@@ -6,6 +6,8 @@
 #include "lif_host.h"
 #include "snn_seq.h"
 
+#include <algorithm>
+
 namespace snnlif {
 
 constexpr int64_t kMaxSeqT = int64_t(1) << 30, kMaxSeqB = int64_t(1) << 24, kMaxSeqF = int64_t(1) << 24;
@@ -149,6 +151,10 @@ inline snn_status check_scan_cfg(const snn_scan_cfg* c) {
 constexpr int kScanStates = 4;   // states per lane
 constexpr int kScanBlock = 8;    // steps that the waves of the local pass share out at a time
 constexpr int64_t kSplitWaves = 1024, kSplitGroups = 128, kSplitSteps = 128, kMaxSegments = 1024;
+// Up to so many segments a workgroup of the scan walks those before its own itself; a kernel that
+// walks them all first costs a launch more and pays behind that (x[4096][1][1024], 64 segments:
+// 60 us to 60 and the launch; x[1000][8][128], 32: 70 to 77; x[4096][1][512], 128: 55 to 48).
+constexpr int64_t kWalkSegments = 64;
 
 // A workgroup owns 64 features of one group and one sequence, a feature per lane; each of its
 // `waves` (a power of two) waves holds 4 of their states.  The forward keeps the state every
@@ -169,10 +175,13 @@ constexpr int64_t scan_held_states(int S) { return int64_t(S + kScanStates - 1) 
 
 // The time axis is cut into segments where the waves of one segment leave SIMDs (1024 of them)
 // without two waves, or its workgroups half the CUs without one: the local pass then costs less
-// than they do idle (x[4096][1][4096] runs in 160 us instead of 624; x[1024][8][4096], which has
+// than they do idle (x[4096][1][4096] runs in 154 us instead of 624; x[1024][8][4096], which has
 // two waves per SIMD, gains nothing).  Four waves per SIMD are aimed for, with segments of 16
-// steps or more (x[333][5][777] of 7 states: forward and backward in 79 us, 114 with 64 or
-// more), once the steps outweigh two more launches.
+// steps or more (forward and backward of x[333][1][777], 7 states: 49 us, 58 with 32 or more),
+// once the steps outweigh another launch.  Walking the segments takes a time per segment and the
+// kernels one per step of them: their sum is least with about sqrt(2 T) segments (forward of
+// x[4096][1][128]: 33 us with 86, 36 with 64 and 44 with 256; x[131072][1][64]: 147 us with 512,
+// 165 with 362 and 164 with 724).
 inline ScanPlan scan_plan(const snn_scan_cfg* c, int64_t T, int64_t B, int64_t F) {
     ScanPlan p;
     p.waves = 1;
@@ -182,7 +191,8 @@ inline ScanPlan scan_plan(const snn_scan_cfg* c, int64_t T, int64_t B, int64_t F
     p.steps = std::max<int64_t>(T, 1);
     p.segments = 1;
     const int64_t groups = p.tiles * c->groups * B, waves = groups * (scan_held_states(c->states) / kScanStates);
-    const int64_t want = std::min(std::min(std::max<int64_t>(4096 / waves, 2), T / 16), kMaxSegments);
+    const int64_t most = std::min({ceil_div(T, 16), int64_t(std::sqrt(2.0 * double(T))), kMaxSegments});
+    const int64_t want = std::min(std::max<int64_t>(4096 / waves, 2), most);
     if ((waves <= kSplitWaves || groups <= kSplitGroups) && T >= kSplitSteps && want > 1) {
         p.steps = ceil_div(ceil_div(T, want), 16) * 16;      // whole blocks, in either direction
         p.segments = ceil_div(T, p.steps);

@@ -84,6 +84,49 @@ struct StateColumn {
     }
 };
 
+// A state that is not finite stays so over a segment, as it does step by step, where the decays
+// of a whole segment multiply to 0 in 32 bits.
+__device__ __forceinline__ float decayed(float decay, float h) {
+    return fabsf(h) < __builtin_inff() ? decay * h : h;
+}
+
+// The state before this segment, or e behind it (DOWN): up to kWalkSegments the workgroup walks
+// the others' states and sums of d itself, more of them the carry kernel has walked.
+template <bool DOWN>
+__device__ __forceinline__ void segment_state(const ScanArgs& a, const ScanPlace& p, const float (&rate)[kSL],
+                                              float (&h)[kSL]) {
+    StateColumn states(a, p, a.part_h);
+    if (a.plan.segments > kWalkSegments) {
+        if (p.states > 0) states.load(blockIdx.y, h);
+        return;
+    }
+    load_state(a, p, DOWN ? a.gh_out : a.h_in, h);
+    if (p.states <= 0) return;
+    const int last = int(a.plan.segments) - 1, n = DOWN ? last - int(blockIdx.y) : int(blockIdx.y);
+    const float* sums = a.part_d + ((DOWN ? last * a.B : 0) + p.b) * a.F + p.f;
+    if (DOWN) states.p += last * states.piece;
+    constexpr int U = 4, DIR = DOWN ? -1 : 1;
+    for (int c0 = 0; c0 < n; c0 += U) {
+        float l[U][kSL], d[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            if (c0 + u < n) {
+                states.load(0, l[u]);
+                d[u] = *sums;
+                states.p += DIR * states.piece;
+                sums += DIR * a.B * a.F;
+            }
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            if (c0 + u < n) {
+#pragma unroll
+                for (int s = 0; s < kSL; ++s) h[s] = decayed(__builtin_amdgcn_exp2f(d[u] * rate[s]), h[s]) + l[u][s];
+            }
+        }
+    }
+}
+
 // The lanes' columns of a [T][B][F] tensor: a row's address is the same for the whole wave and
 // stays in scalar registers, a lane adds the offset of its feature.
 template <int IO>

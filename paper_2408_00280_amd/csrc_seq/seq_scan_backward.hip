@@ -63,16 +63,20 @@ __global__ __launch_bounds__(NS * kWave, NS > 8 ? 4 : 2) void scan_backward_kern
     float rate[kSL], e[kSL], gA[kSL], gD = 0.0f, gbias = 0.0f;
     load_rates(a, p, rate);
     // Lanes behind the group's last feature have steps and states of 0 and add nothing.
-    const auto load = [&](const float* first, const StateColumn& kept, int64_t c, bool at_first, float (&v)[kSL]) {
+    const StateColumn kept(a, p, a.saved);
+    const auto load = [&](int64_t c, bool first, float (&v)[kSL]) {
 #pragma unroll
         for (int s = 0; s < kSL; ++s) v[s] = 0.0f;
         if (!p.active) return;
-        if (at_first) load_state(a, p, first, v);
+        if (first) load_state(a, p, a.h_in, v);
         else if (p.states > 0) kept.load(c, v);
     };
-    load(a.gh_out, StateColumn(a, p, a.part_h), blockIdx.y, a.plan.segments == 1, e);
+    segment_state<true>(a, p, rate, e);
 #pragma unroll
-    for (int i = 0; i < kSL; ++i) gA[i] = 0.0f;
+    for (int i = 0; i < kSL; ++i) {
+        gA[i] = 0.0f;
+        if (!p.active) e[i] = 0.0f;
+    }
     float skip = a.D != nullptr ? a.D[p.f] : 0.0f, bias = a.dt_bias != nullptr ? a.dt_bias[p.f] : 0.0f;
     const Columns<IO> cx(a.x, p), cdt(a.dt, p), cgy(a.gy, p), cgx(a.gx, p), cgdt(a.gdt, p);
     const bool busy = p.states > 0;
@@ -106,7 +110,6 @@ __global__ __launch_bounds__(NS * kWave, NS > 8 ? 4 : 2) void scan_backward_kern
             }
         }
     };
-    const StateColumn kept(a, p, a.saved);
 
     int t0 = p.t0 + (p.t1 - 1 - p.t0) / K * K;
     for (; t0 >= p.t0 && t0 >= p.len; t0 -= K) {     // blocks behind the sequence's end
@@ -138,7 +141,7 @@ __global__ __launch_bounds__(NS * kWave, NS > 8 ? 4 : 2) void scan_backward_kern
         const f32x4_t* bc = reinterpret_cast<const f32x4_t*>(m.sbc[block].v[k][p.wave]);
         return Ahead{m.sd[block][k][p.lane], bc[0], bc[1]};
     };
-    load(a.h_in, kept, t0 / K - 1, t0 <= 0, h);
+    load(t0 / K - 1, t0 <= 0, h);
     settle(skip);
     settle(bias);
     settle(rate);
@@ -176,7 +179,7 @@ __global__ __launch_bounds__(NS * kWave, NS > 8 ? 4 : 2) void scan_backward_kern
                 if (kAhead && k > 0) ahead = read(buf, k - 1);
                 if (!kAhead) step = read(buf, k);
                 if (k == K / 2) {                // half of the block's registers are free by now
-                    load(a.h_in, kept, below / K - 1, below == 0, h_next);
+                    load(below / K - 1, below == 0, h_next);
                 }
                 __builtin_amdgcn_sched_barrier(0);
                 if (k < K - 1) sum_up(k + 1);

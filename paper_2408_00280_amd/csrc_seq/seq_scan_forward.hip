@@ -22,8 +22,7 @@ __global__ __launch_bounds__(NS * kWave) void scan_forward_kernel(ScanArgs a) {
     const ScanPlace p = scan_place(a);
     float rate[kSL], h[kSL];
     load_rates(a, p, rate);
-    if (a.plan.segments == 1) load_state(a, p, a.h_in, h);
-    else if (p.states > 0) StateColumn(a, p, a.part_h).load(blockIdx.y, h);
+    segment_state<false>(a, p, rate, h);
     float skip = a.D != nullptr ? a.D[p.f] : 0.0f, bias = a.dt_bias != nullptr ? a.dt_bias[p.f] : 0.0f;
     settle(skip);
     settle(bias);
@@ -146,8 +145,7 @@ __global__ __launch_bounds__(kWave) void scan_forward_one_kernel(ScanArgs a) {
     const ScanPlace p = scan_place(a);
     float rate[kSL], h[kSL];
     load_rates(a, p, rate);
-    if (a.plan.segments == 1) load_state(a, p, a.h_in, h);
-    else StateColumn(a, p, a.part_h).load(blockIdx.y, h);
+    segment_state<false>(a, p, rate, h);
     float skip = a.D != nullptr ? a.D[p.f] : 0.0f, bias = a.dt_bias != nullptr ? a.dt_bias[p.f] : 0.0f;
     settle(skip);
     settle(bias);
