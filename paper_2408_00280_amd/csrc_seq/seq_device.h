@@ -87,6 +87,26 @@ __device__ __forceinline__ float wave_sum(float v) {
     return __uint_as_float(b[0]) + __uint_as_float(b[1]);
 }
 
+// Sums of partial results: a workgroup's 64 values, its waves over the partial results.
+__device__ __forceinline__ void reduce_partials(const float* part, int64_t P, int64_t stride, const ReduceOut& out,
+                                                int64_t block, float (*lds)[kWave]) {
+    const int lane = threadIdx.x & (kWave - 1), wave = threadIdx.x / kWave, waves = blockDim.x / kWave;
+    int64_t i = block * kWave + lane;
+    const bool in = i < out.n[0] + out.n[1] + out.n[2];
+    float s = 0.0f;
+    if (in) {
+#pragma unroll 8
+        for (int64_t p = wave; p < P; p += waves) s += part[p * stride + i];
+    }
+    lds[wave][lane] = s;
+    __syncthreads();
+    if (wave != 0 || !in) return;
+    for (int w = 1; w < waves; ++w) s += lds[w][lane];
+    int k = 0;
+    while (i >= out.n[k]) i -= out.n[k++];
+    if (out.p[k] != nullptr) out.p[k][i] = s;
+}
+
 // A barrier that orders the LDS only: loads from memory stay in flight over it.
 __device__ __forceinline__ void lds_barrier() {
     __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup", "local");

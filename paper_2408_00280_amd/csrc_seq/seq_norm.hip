@@ -532,24 +532,9 @@ __global__ __launch_bounds__(kLongLanes) void norm_long_backward_kernel(NormArgs
     }
 }
 
-// 64 values per workgroup, its waves over the partial results.
 __global__ __launch_bounds__(1024) void reduce_kernel(const float* part, int64_t P, int64_t stride, ReduceOut out) {
     __shared__ float lds[16][kWave];
-    const int lane = threadIdx.x & (kWave - 1), wave = threadIdx.x / kWave, waves = blockDim.x / kWave;
-    int64_t i = int64_t(blockIdx.x) * kWave + lane;
-    const bool in = i < out.n[0] + out.n[1] + out.n[2];
-    float s = 0.0f;
-    if (in) {
-#pragma unroll 8
-        for (int64_t p = wave; p < P; p += waves) s += part[p * stride + i];
-    }
-    lds[wave][lane] = s;
-    __syncthreads();
-    if (wave != 0 || !in) return;
-    for (int w = 1; w < waves; ++w) s += lds[w][lane];
-    int k = 0;
-    while (i >= out.n[k]) i -= out.n[k++];
-    if (out.p[k] != nullptr) out.p[k][i] = s;
+    reduce_partials(part, P, stride, out, blockIdx.x, lds);
 }
 
 }  // namespace

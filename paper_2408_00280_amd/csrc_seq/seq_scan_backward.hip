@@ -265,10 +265,16 @@ __global__ __launch_bounds__(NS * kWave, NS > 8 ? 4 : 2) void scan_backward_kern
     }
 }
 
-// dL/dB and dL/dC: the sums over a group's tiles.
+// The sums of the partial results: those of dL/dA, dL/dD and dL/d(dt_bias) over segments and
+// sequences in the first `reduce` workgroups, dL/dB and dL/dC over a group's tiles in the others.
+constexpr int kJoin = 1024;
+
 template <int IO>
-__global__ __launch_bounds__(kBlock) void scan_join_kernel(ScanArgs a, int64_t n) {
-    const int64_t i = int64_t(blockIdx.x) * kBlock + threadIdx.x;
+__global__ __launch_bounds__(kJoin) void scan_join_kernel(ScanArgs a, ReduceOut out, int64_t reduce, int64_t n) {
+    __shared__ float lds[kJoin / kWave][kWave];
+    if (blockIdx.x < reduce)
+        return reduce_partials(a.part_f, a.plan.segments * a.B, scan_partial_values(a.F, a.S), out, blockIdx.x, lds);
+    const int64_t i = (blockIdx.x - reduce) * kJoin + threadIdx.x;
     if (i >= n) return;
     const int waves = a.plan.waves, s = int(i % a.S);
     const int64_t q = i / a.S, which = q & 1, r = q >> 1;
@@ -305,12 +311,11 @@ snn_status backward_states(const ScanArgs& a, hipStream_t s) {
 
 template <int IO>
 snn_status backward_io(const ScanArgs& a, hipStream_t s) {
-    snn_status st = a.S % kSL == 0 ? backward_states<IO, true>(a, s) : backward_states<IO, false>(a, s);
+    const snn_status st = a.S % kSL == 0 ? backward_states<IO, true>(a, s) : backward_states<IO, false>(a, s);
     if (st != SNN_OK) return st;
-    const int64_t n = a.T * a.B * a.G * 2 * a.S;
-    if ((st = launch(scan_join_kernel<IO>, grid_for(n), s, a, n)) != SNN_OK) return st;
     const ReduceOut out = {{a.gA, a.gD, a.gdt_bias}, {a.F * a.S, a.F, a.F}};
-    return reduce_entry(a.part_f, a.plan.segments * a.B, scan_partial_values(a.F, a.S), out, s);
+    const int64_t reduce = ceil_div(scan_partial_values(a.F, a.S), kWave), n = a.T * a.B * a.G * 2 * a.S;
+    return launch_blk(scan_join_kernel<IO>, dim3(unsigned(reduce + ceil_div(n, kJoin))), kJoin, s, a, out, reduce, n);
 }
 
 }  // namespace
