@@ -138,7 +138,7 @@ def _ptr(a):
     if a is None:
         return None
     if isinstance(a, torch.Tensor):
-        if a.numel() and not a.is_contiguous():
+        if not a.is_contiguous() and a.numel():
             raise ValueError("tensor arguments must be contiguous")
         return a.data_ptr() or None
     return int(a)

@@ -22,8 +22,26 @@ from . import native
 IO_OF = {torch.float32: native.SNN_IO_F32, torch.bfloat16: native.SNN_IO_BF16}
 ACTS = {None: native.SNN_ACT_NONE, "silu": native.SNN_ACT_SILU}
 
-_conv_cfg, _scan_cfg, _norm_cfg = (functools.lru_cache(maxsize=64)(c) for c in (
-    native.snn_conv_cfg, native.snn_scan_cfg, native.snn_norm_cfg))
+
+# Configurations with the bytes of saved data and workspaces, which depend on nothing but
+# configuration and shape: a call finds them in a dictionary instead of asking for them.
+
+@functools.lru_cache(maxsize=256)
+def _conv_plan(io, W, act, T, B, F):
+    cfg = native.snn_conv_cfg(io, W, act)
+    return cfg, native.snn_conv_workspace_bytes(cfg, T, B, F)
+
+
+@functools.lru_cache(maxsize=256)
+def _scan_plan(io, S, G, softplus, T, B, F):
+    cfg = native.snn_scan_cfg(io, S, G, softplus)
+    return cfg, native.snn_scan_saved_bytes(cfg, T, B, F), *native.snn_scan_workspace_bytes(cfg, T, B, F)
+
+
+@functools.lru_cache(maxsize=256)
+def _norm_plan(io, eps, T, B, F):
+    cfg = native.snn_norm_cfg(io, eps)
+    return cfg, native.snn_norm_workspace_bytes(cfg, T, B, F)
 
 
 def _on_stream(fn):
@@ -73,9 +91,12 @@ def _data(name, a, x, shape):
 
 
 def _dense(name, a, x, shape, dtype=torch.float32):
-    if a is not None and (a.dtype != dtype or a.shape != shape or not a.is_contiguous()
-                          or a.get_device() != x.get_device()):
+    """The address of a parameter, a state or lengths; None without one."""
+    if a is None:
+        return None
+    if a.dtype != dtype or a.shape != shape or not a.is_contiguous() or a.get_device() != x.get_device():
         raise ValueError(f"{name} must be a contiguous {dtype} tensor of shape {tuple(shape)} on {x.device}")
+    return a.data_ptr() or None
 
 
 def _bytes(n, x):
@@ -101,11 +122,9 @@ def _conv_args(x, weight, bias, act, state, lengths):
         raise ValueError("weight must be [F, W], act None or 'silu'")
     W = weight.shape[1]
     x = _rows(x)
-    _dense("weight", weight, x, (F, W))
-    _dense("bias", bias, x, (F,))
-    _dense("state", state, x, (W - 1, B, F), x.dtype)
-    _dense("lengths", lengths, x, (B,), torch.int32)
-    return x, T, B, F, W, _conv_cfg(IO_OF[x.dtype], W, ACTS[act])
+    args = (x, _dense("weight", weight, x, (F, W)), _dense("bias", bias, x, (F,)),
+            _dense("state", state, x, (W - 1, B, F), x.dtype), _dense("lengths", lengths, x, (B,), torch.int32))
+    return args, (T, B, F, W), _conv_plan(IO_OF[x.dtype], W, ACTS[act], T, B, F)
 
 
 @_on_stream
@@ -113,11 +132,12 @@ def conv_forward(x, weight, bias=None, *, act="silu", state=None, state_out=None
     """Causal convolution of x[T, B, F] along time with weight[F, W] (W up to 8, the last tap
     on the current step), bias[F] and activation: y.  state ([W-1, B, F]): the inputs before
     step 0; state_out: written with the last W-1 inputs, may be `state` (in place)."""
-    x, T, B, F, W, cfg = _conv_args(x, weight, bias, act, state, lengths)
-    _dense("state_out", state_out, x, (W - 1, B, F), x.dtype)
+    args, (T, B, F, W), (cfg, _) = _conv_args(x, weight, bias, act, state, lengths)
+    x = args[0]
+    out = _dense("state_out", state_out, x, (W - 1, B, F), x.dtype)
     y = torch.empty_like(x)
-    if x.numel():
-        native.snn_conv_forward(cfg, T, B, F, x, weight, bias, state, lengths, y, state_out)
+    if T and B and F:
+        native.snn_conv_forward(cfg, T, B, F, *args, y, out)
     else:
         _hand_over(state_out, state)
     return y
@@ -127,17 +147,17 @@ def conv_forward(x, weight, bias=None, *, act="silu", state=None, state_out=None
 def conv_backward(x, weight, bias, grad_y, *, act="silu", state=None, lengths=None, grad_state_out=None):
     """Gradients (x, weight, bias or None, state or None) of conv_forward with the same
     arguments; grad_state_out: the gradient of its state_out."""
-    x, T, B, F, W, cfg = _conv_args(x, weight, bias, act, state, lengths)
+    args, (T, B, F, W), (cfg, ws) = _conv_args(x, weight, bias, act, state, lengths)
+    x = args[0]
     gy = _data("grad_y", grad_y, x, (T, B, F))
-    _dense("grad_state_out", grad_state_out, x, (W - 1, B, F), x.dtype)
-    empty = not x.numel()
+    g_out = _dense("grad_state_out", grad_state_out, x, (W - 1, B, F), x.dtype)
+    empty = not (T and B and F)
     gx, gw, gb = torch.empty_like(x), _params(weight, empty), _params(bias, empty)
     gs = None if state is None else torch.empty_like(state)
     if empty:
         _hand_over(gs, grad_state_out)
     else:
-        ws = _bytes(native.snn_conv_workspace_bytes(cfg, T, B, F), x)
-        native.snn_conv_backward(cfg, T, B, F, x, weight, bias, state, lengths, gy, grad_state_out, gx, gw, gb, gs, ws)
+        native.snn_conv_backward(cfg, T, B, F, *args, gy, g_out, gx, gw, gb, gs, _bytes(ws, x))
     return gx, gw, gb, gs
 
 
@@ -150,13 +170,9 @@ def _scan_args(x, dt, A, Bm, Cm, D, dt_bias, softplus, h_in, lengths):
     G, S = Bm.shape[2:]
     x, dt = _rows(x), _data("dt", dt, x, (T, B, F))
     Bm, Cm = _data("Bm", Bm, x, (T, B, G, S)), _data("Cm", Cm, x, (T, B, G, S))
-    _dense("A", A, x, (F, S))
-    _dense("D", D, x, (F,))
-    _dense("dt_bias", dt_bias, x, (F,))
-    _dense("h_in", h_in, x, (B, F, S))
-    _dense("lengths", lengths, x, (B,), torch.int32)
-    cfg = _scan_cfg(IO_OF[x.dtype], S, G, int(bool(softplus)))
-    return (x, dt, A, Bm, Cm, D, dt_bias, h_in, lengths), (T, B, F, G, S), cfg
+    args = (x, dt, _dense("A", A, x, (F, S)), Bm, Cm, _dense("D", D, x, (F,)), _dense("dt_bias", dt_bias, x, (F,)),
+            _dense("h_in", h_in, x, (B, F, S)), _dense("lengths", lengths, x, (B,), torch.int32))
+    return args, (T, B, F, S), _scan_plan(IO_OF[x.dtype], S, G, int(bool(softplus)), T, B, F)
 
 
 @_on_stream
@@ -167,16 +183,15 @@ def scan_forward(x, dt, A, Bm, Cm, D=None, dt_bias=None, *, softplus=True, h_in=
     skip weights D [F].  h_in, h_out ([B, F, S] float32): the state before step 0 and after
     the last, h_out is written and may be h_in (in place).  Returns (y, saved), saved for
     scan_backward with train=True and None otherwise."""
-    args, (T, B, F, G, S), cfg = _scan_args(x, dt, A, Bm, Cm, D, dt_bias, softplus, h_in, lengths)
+    args, (T, B, F, S), (cfg, kept, ws, _) = _scan_args(x, dt, A, Bm, Cm, D, dt_bias, softplus, h_in, lengths)
     x = args[0]
-    _dense("h_out", h_out, x, (B, F, S))
-    if train and h_out is not None and h_in is not None and h_out.data_ptr() == h_in.data_ptr() and h_in.numel():
+    out = _dense("h_out", h_out, x, (B, F, S))
+    if train and out is not None and out == args[7]:
         raise ValueError("the backward reads h_in: h_out must be another tensor")
     y = torch.empty_like(x)
-    saved = x.new_empty(native.snn_scan_saved_bytes(cfg, T, B, F), dtype=torch.uint8) if train else None
-    if x.numel():
-        ws = _bytes(native.snn_scan_workspace_bytes(cfg, T, B, F)[0], x)
-        native.snn_scan_forward(cfg, T, B, F, *args, y, h_out, saved if train and saved.numel() else None, ws)
+    saved = x.new_empty(kept, dtype=torch.uint8) if train else None
+    if T and B and F:
+        native.snn_scan_forward(cfg, T, B, F, *args, y, out, saved if train and kept else None, _bytes(ws, x))
     else:
         _hand_over(h_out, h_in)
     return y, saved
@@ -187,14 +202,14 @@ def scan_backward(x, dt, A, Bm, Cm, D, dt_bias, saved, grad_y, *, softplus=True,
                   grad_h_out=None):
     """Gradients (x, dt, A, Bm, Cm, D or None, dt_bias or None, h_in or None) of scan_forward
     with the same arguments and what it saved; grad_h_out: the gradient of its h_out."""
-    args, (T, B, F, G, S), cfg = _scan_args(x, dt, A, Bm, Cm, D, dt_bias, softplus, h_in, lengths)
+    args, (T, B, F, S), (cfg, kept, _, ws) = _scan_args(x, dt, A, Bm, Cm, D, dt_bias, softplus, h_in, lengths)
     x = args[0]
     if saved is None:
         raise ValueError("saved must be what scan_forward(train=True) returned for these arguments")
-    _dense("saved", saved, x, (native.snn_scan_saved_bytes(cfg, T, B, F),), torch.uint8)
+    saved = _dense("saved", saved, x, (kept,), torch.uint8)
     gy = _data("grad_y", grad_y, x, (T, B, F))
-    _dense("grad_h_out", grad_h_out, x, (B, F, S))
-    empty = not x.numel()
+    g_out = _dense("grad_h_out", grad_h_out, x, (B, F, S))
+    empty = not (T and B and F)
     gx, gdt, gB, gC = torch.empty_like(x), torch.empty_like(x), torch.empty_like(args[3]), torch.empty_like(args[4])
     gA, gD, gbias = _params(A, empty), _params(D, empty), _params(dt_bias, empty)
     gh = None if h_in is None else torch.empty_like(h_in)
@@ -202,9 +217,8 @@ def scan_backward(x, dt, A, Bm, Cm, D, dt_bias, saved, grad_y, *, softplus=True,
         gB.zero_(), gC.zero_()
         _hand_over(gh, grad_h_out)
     else:
-        ws = _bytes(native.snn_scan_workspace_bytes(cfg, T, B, F)[1], x)
-        native.snn_scan_backward(cfg, T, B, F, *args, saved if saved.numel() else None, gy, grad_h_out, gx, gdt, gA, gB,
-                                 gC, gD, gbias, gh, ws)
+        native.snn_scan_backward(cfg, T, B, F, *args, saved, gy, g_out, gx, gdt, gA, gB, gC, gD, gbias, gh,
+                                 _bytes(ws, x))
     return gx, gdt, gA, gB, gC, gD, gbias, gh
 
 
@@ -215,10 +229,9 @@ def _norm_args(y, r, z, w_post, scale, w_pre, eps, lengths):
     y = _rows(y)
     r = None if r is None else _data("r", r, y, (T, B, F))
     z = None if z is None else _data("z", z, y, (T, B, F))
-    for name, w in (("w_post", w_post), ("scale", scale), ("w_pre", w_pre)):
-        _dense(name, w, y, (F,))
-    _dense("lengths", lengths, y, (B,), torch.int32)
-    return (y, z, r, w_post, scale, w_pre, lengths), (T, B, F), _norm_cfg(IO_OF[y.dtype], eps)
+    args = (y, z, r, _dense("w_post", w_post, y, (F,)), _dense("scale", scale, y, (F,)),
+            _dense("w_pre", w_pre, y, (F,)), _dense("lengths", lengths, y, (B,), torch.int32))
+    return args, (T, B, F), _norm_plan(IO_OF[y.dtype], eps, T, B, F)
 
 
 @_on_stream
@@ -227,10 +240,10 @@ def norm_forward(y, r=None, z=None, w_post=None, scale=None, w_pre=None, *, eps=
     r_new = r + scale * norm(y * silu(z)) and u = norm(r_new), root-mean-square norms with the
     weights w_post and w_pre.  Without z, w_post, scale, r or w_pre that part is left out.
     Returns (r_new, u or None, rstd), rstd for norm_backward with train=True, else None."""
-    args, (T, B, F), cfg = _norm_args(y, r, z, w_post, scale, w_pre, eps, lengths)
+    args, (T, B, F), (cfg, _) = _norm_args(y, r, z, w_post, scale, w_pre, eps, lengths)
     r_new, u = torch.empty_like(args[0]), None if w_pre is None else torch.empty_like(args[0])
     rstd = torch.empty((2, T, B), dtype=torch.float32, device=y.device) if train else None
-    if y.numel():
+    if T and B and F:
         native.snn_norm_forward(cfg, T, B, F, *args, r_new, u, rstd)
     return r_new, u, rstd
 
@@ -239,15 +252,14 @@ def norm_forward(y, r=None, z=None, w_post=None, scale=None, w_pre=None, *, eps=
 def norm_backward(y, r, z, w_post, scale, w_pre, rstd, grad_r_new, grad_u=None, *, eps=1e-5, lengths=None):
     """Gradients (y, r, z, w_post, scale, w_pre; None where the input is None) of norm_forward
     with the same arguments and its rstd.  grad_r_new or grad_u may be None (no gradient)."""
-    args, (T, B, F), cfg = _norm_args(y, r, z, w_post, scale, w_pre, eps, lengths)
+    args, (T, B, F), (cfg, ws) = _norm_args(y, r, z, w_post, scale, w_pre, eps, lengths)
     y = args[0]
-    _dense("rstd", rstd, y, (2, T, B))
+    rstd = _dense("rstd", rstd, y, (2, T, B))
     g1 = None if grad_r_new is None else _data("grad_r_new", grad_r_new, y, (T, B, F))
     g2 = None if grad_u is None else _data("grad_u", grad_u, y, (T, B, F))
-    empty = not y.numel()
+    empty = not (T and B and F)
     gy, gr, gz = (None if a is None else torch.empty_like(a) for a in (args[0], args[2], args[1]))
     gw = [_params(w, empty) for w in (w_post, scale, w_pre)]
     if not empty:
-        ws = _bytes(native.snn_norm_workspace_bytes(cfg, T, B, F), y)
-        native.snn_norm_backward(cfg, T, B, F, *args, rstd, g1, g2, gy, gz, gr, *gw, ws)
+        native.snn_norm_backward(cfg, T, B, F, *args, rstd, g1, g2, gy, gz, gr, *gw, _bytes(ws, y))
     return gy, gr, gz, *gw
