@@ -19,9 +19,9 @@ from __future__ import annotations
 import math
 
 import torch
-from torch.autograd.function import once_differentiable
 
 from . import layer, sequence
+from .sequence import _sequence
 
 _IO = {torch.float32: "f32", torch.bfloat16: "bf16"}
 
@@ -177,36 +177,11 @@ class LIFStack(torch.nn.Module):
                 f"v_th={self.v_th}, v_reset={self.v_reset}, alpha={self.alpha}, reset={self.reset}")
 
 
-class FusedConv(torch.autograd.Function):
-    """sequence.conv_forward / conv_backward; the outputs are y and the last W-1 inputs."""
-
-    @staticmethod
-    def forward(ctx, x, weight, bias, state, lengths, act, want_state):
-        W = weight.shape[1]
-        out = torch.empty((W - 1, *x.shape[1:]), dtype=x.dtype, device=x.device) if want_state else None
-        y = sequence.conv_forward(x, weight, bias, act=act, state=state, state_out=out, lengths=lengths)
-        ctx.save_for_backward(x, weight, bias, state, lengths)
-        ctx.act = act
-        ctx.set_materialize_grads(False)
-        return y, out
-
-    @staticmethod
-    @once_differentiable
-    def backward(ctx, grad_y, grad_state_out):
-        x, weight, bias, state, lengths = ctx.saved_tensors
-        grad_y = torch.zeros_like(x) if grad_y is None else grad_y
-        if grad_state_out is not None:
-            grad_state_out = grad_state_out.contiguous()
-        g = sequence.conv_backward(x, weight, bias, grad_y, act=ctx.act, state=state, lengths=lengths,
-                                   grad_state_out=grad_state_out)
-        return (*g, None, None, None)
-
-
 def causal_conv(x, weight, bias=None, *, act="silu", state=None, lengths=None, return_state=False):
     """Short causal convolution of x[T, B, F] along time (see sequence.conv_forward), with
     gradients for x, weight, bias and state.  Returns y, or (y, the last W-1 inputs)."""
-    y, out = FusedConv.apply(x, weight, bias, state, lengths, act, return_state)
-    return (y, out) if return_state else y
+    out = _sequence.causal_conv(x, weight, bias, sequence.act_code(act), state, lengths, return_state)
+    return out if return_state else out[0]
 
 
 class CausalConv(torch.nn.Module):
@@ -235,37 +210,12 @@ class CausalConv(torch.nn.Module):
         return f"features={self.weight.shape[0]}, width={self.weight.shape[1]}, act={self.act}"
 
 
-class FusedScan(torch.autograd.Function):
-    """sequence.scan_forward / scan_backward; the outputs are y and the state after the last step."""
-
-    @staticmethod
-    def forward(ctx, x, dt, A, Bm, Cm, D, dt_bias, h_in, lengths, softplus, want_state):
-        out = torch.empty((x.shape[1], *A.shape), dtype=torch.float32, device=x.device) if want_state else None
-        y, saved = sequence.scan_forward(x, dt, A, Bm, Cm, D, dt_bias, softplus=softplus, h_in=h_in, h_out=out,
-                                         lengths=lengths, train=any(ctx.needs_input_grad))
-        ctx.save_for_backward(x, dt, A, Bm, Cm, D, dt_bias, h_in, lengths, saved)
-        ctx.softplus = softplus
-        ctx.set_materialize_grads(False)
-        return y, out
-
-    @staticmethod
-    @once_differentiable
-    def backward(ctx, grad_y, grad_h_out):
-        *args, h_in, lengths, saved = ctx.saved_tensors
-        grad_y = torch.zeros_like(args[0]) if grad_y is None else grad_y
-        if grad_h_out is not None:
-            grad_h_out = grad_h_out.contiguous()
-        g = sequence.scan_backward(*args, saved, grad_y, softplus=ctx.softplus, h_in=h_in, lengths=lengths,
-                                   grad_h_out=grad_h_out)
-        return (*g, None, None, None)
-
-
 def selective_scan(x, dt, A, Bm, Cm, D=None, dt_bias=None, *, softplus=True, h_in=None, lengths=None,
                    return_state=False):
     """Selective state space scan of x[T, B, F] (see sequence.scan_forward), with gradients for
     every input.  Returns y, or (y, the state [B, F, S] after the last step)."""
-    y, out = FusedScan.apply(x, dt, A, Bm, Cm, D, dt_bias, h_in, lengths, softplus, return_state)
-    return (y, out) if return_state else y
+    out = _sequence.selective_scan(x, dt, A, Bm, Cm, D, dt_bias, bool(softplus), h_in, lengths, return_state)
+    return out if return_state else out[0]
 
 
 class SelectiveScan(torch.nn.Module):
@@ -300,29 +250,11 @@ class SelectiveScan(torch.nn.Module):
         return f"features={self.A_log.shape[0]}, states={self.A_log.shape[1]}"
 
 
-class FusedBlockNorm(torch.autograd.Function):
-    """sequence.norm_forward / norm_backward."""
-
-    @staticmethod
-    def forward(ctx, y, r, z, w_post, scale, w_pre, lengths, eps):
-        r_new, u, rstd = sequence.norm_forward(y, r, z, w_post, scale, w_pre, eps=eps, lengths=lengths,
-                                               train=any(ctx.needs_input_grad))
-        ctx.save_for_backward(y, r, z, w_post, scale, w_pre, rstd, lengths)
-        ctx.eps = eps
-        ctx.set_materialize_grads(False)
-        return r_new, u
-
-    @staticmethod
-    @once_differentiable
-    def backward(ctx, grad_r_new, grad_u):
-        *args, lengths = ctx.saved_tensors
-        return (*sequence.norm_backward(*args, grad_r_new, grad_u, eps=ctx.eps, lengths=lengths), None, None)
-
-
 def block_norm(y, r=None, z=None, w_post=None, scale=None, w_pre=None, *, eps=1e-5, lengths=None):
     """A block's gate, norm and scaled residual with the next block's norm (see
     sequence.norm_forward), with gradients for every input: (r_new, u or None)."""
-    return FusedBlockNorm.apply(y, r, z, w_post, scale, w_pre, lengths, eps)
+    out = _sequence.block_norm(y, r, z, w_post, scale, w_pre, lengths, eps)
+    return out[0], out[1] if w_pre is not None else None
 
 
 class BlockNorm(torch.nn.Module):

@@ -259,6 +259,55 @@ def test_rates_whose_exponent_is_past_the_type(ops, T, S):
         ops.scan_backward(x, step, A, Bm, Cm, D, bias, None, gy, h_in=h, lengths=ln, grad_h_out=gh)
 
 
+def test_gradients_are_differentiated_once(ops):
+    """A second backward through a gradient raises an error: it is no constant."""
+    from paper_2408_00280_amd import autograd
+    x, step, A, Bm, Cm, *_ = scan_inputs("f32", 5, 2, 66, 4, 1, "")
+    w = normal(9, 66, 4)
+    for run in (lambda v: autograd.causal_conv(v, w), lambda v: autograd.selective_scan(v, step, A, Bm, Cm),
+                lambda v: autograd.block_norm(v, w_pre=w[:, 0].contiguous())[1]):
+        v = x.clone().requires_grad_(True)
+        g, = torch.autograd.grad(run(v).square().sum(), v, create_graph=True)
+        assert g.requires_grad
+        with pytest.raises(RuntimeError):
+            g.sum().backward()
+        plain_g, = torch.autograd.grad(run(v).square().sum(), v)
+        assert not plain_g.requires_grad and torch.equal(plain_g, g.detach())
+
+
+def test_a_state_written_behind_a_graph_is_noticed(ops):
+    """A state that a graph keeps for its backward and a later call updates in place."""
+    from paper_2408_00280_amd import autograd
+    x, step, A, Bm, Cm, _, _, h, *_ = scan_inputs("f32", 5, 2, 66, 4, 1, "h")
+    w, state = normal(9, 66, 4), normal(10, 3, 2, 66)
+    x.requires_grad_(True)
+    y = autograd.selective_scan(x, step, A, Bm, Cm, h_in=h)
+    ops.scan_forward(x.detach(), step, A, Bm, Cm, h_in=h, h_out=h)
+    with pytest.raises(RuntimeError, match="inplace"):
+        y.sum().backward()
+    y = autograd.causal_conv(x, w, state=state)
+    ops.conv_forward(x.detach(), w, state=state, state_out=state)
+    with pytest.raises(RuntimeError, match="inplace"):
+        y.sum().backward()
+
+
+def test_what_autograd_refuses(ops):
+    """Wrong arguments raise the same errors as without gradients."""
+    from paper_2408_00280_amd import autograd
+    from paper_2408_00280_amd.native import SnnError
+    x, step, A, Bm, Cm, *_ = scan_inputs("f32", 5, 2, 66, 4, 1, "")
+    v = x.clone().requires_grad_(True)
+    for call in (lambda: autograd.causal_conv(v, A[:, 0]), lambda: autograd.causal_conv(v, A, act="relu"),
+                 lambda: autograd.causal_conv(v.cpu(), A), lambda: autograd.selective_scan(v, step[:3], A, Bm, Cm),
+                 lambda: autograd.selective_scan(v, step, A.bfloat16(), Bm, Cm), lambda: autograd.block_norm(v, x[:3]),
+                 lambda: autograd.selective_scan(v, step, A, Bm, Cm, h_in=A)):
+        with pytest.raises(ValueError):
+            call()
+    for call in (lambda: autograd.causal_conv(v, normal(8, 66, 9)), lambda: autograd.block_norm(v, eps=0.0)):
+        with pytest.raises(SnnError):
+            call()
+
+
 def test_block_captured_through_autograd(ops):
     """A block's forward and gradients captured into a graph with no eager graph of its leaves
     alive; every replay, with new inputs and other work in between, gives the eager values."""
