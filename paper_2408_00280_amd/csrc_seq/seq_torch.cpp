@@ -126,7 +126,7 @@ struct ConvCall {
     int32_t* lengths;
     ConvCall(const Tensor& x_, const Tensor& w, const Tensor& b, int64_t act, const Tensor& st, const Tensor& ln) {
         const int io = io_of(x_);
-        if (w.dim() != 2 || (act != SNN_ACT_NONE && act != SNN_ACT_SILU))
+        if (!w.defined() || w.dim() != 2 || (act != SNN_ACT_NONE && act != SNN_ACT_SILU))
             refuse("weight must be [F, W], act None or 'silu'");
         x = rows(x_);
         T = x.size(0), B = x.size(1), F = x.size(2), W = w.size(1);
@@ -190,7 +190,8 @@ struct ScanCall {
     ScanCall(const Tensor& x_, const Tensor& dt_, const Tensor& A_, const Tensor& Bm_, const Tensor& Cm_, const Tensor& D_,
              const Tensor& dt_bias_, bool softplus, const Tensor& h, const Tensor& ln) {
         const int io = io_of(x_);
-        if (Bm_.dim() != 4 || A_.dim() != 2) refuse("A must be [F, S], Bm and Cm [T, B, G, S]");
+        if (!A_.defined() || !Bm_.defined() || Bm_.dim() != 4 || A_.dim() != 2)
+            refuse("A must be [F, S], Bm and Cm [T, B, G, S]");
         x = rows(x_);
         T = x.size(0), B = x.size(1), F = x.size(2), G = Bm_.size(2), S = Bm_.size(3);
         dt = data("dt", dt_, x, {T, B, F});
@@ -365,7 +366,7 @@ struct Conv : torch::autograd::Function<Conv> {
 variable_list causal_conv(const Tensor& x, const Tensor& weight, const Optional& bias, int64_t act, const Optional& state,
                           const Optional& lengths, bool want_state) {
     io_of(x);
-    if (weight.dim() != 2 || weight.size(1) < 1) refuse("weight must be [F, W], act None or 'silu'");
+    if (!weight.defined() || weight.dim() != 2 || weight.size(1) < 1) refuse("weight must be [F, W], act None or 'silu'");
     if (any_requires_grad({x, weight, or_none(bias), or_none(state)}))
         return Conv::apply(x, weight, bias, state, lengths, act, want_state);
     Tensor out;
@@ -399,7 +400,8 @@ variable_list selective_scan(const Tensor& x, const Tensor& dt, const Tensor& A,
                              const Optional& D, const Optional& dt_bias, bool softplus, const Optional& h_in,
                              const Optional& lengths, bool want_state) {
     io_of(x);
-    if (A.dim() != 2) refuse("A must be [F, S], Bm and Cm [T, B, G, S]");
+    if (!dt.defined() || !A.defined() || A.dim() != 2 || !Bm.defined() || !Cm.defined())
+        refuse("dt must be [T, B, F], A [F, S], Bm and Cm [T, B, G, S]");
     if (any_requires_grad({x, dt, A, Bm, Cm, or_none(D), or_none(dt_bias), or_none(h_in)}))
         return Scan::apply(x, dt, A, Bm, Cm, D, dt_bias, h_in, lengths, softplus, want_state);
     Tensor out;

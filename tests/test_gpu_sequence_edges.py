@@ -300,7 +300,11 @@ def test_what_autograd_refuses(ops):
     for call in (lambda: autograd.causal_conv(v, A[:, 0]), lambda: autograd.causal_conv(v, A, act="relu"),
                  lambda: autograd.causal_conv(v.cpu(), A), lambda: autograd.selective_scan(v, step[:3], A, Bm, Cm),
                  lambda: autograd.selective_scan(v, step, A.bfloat16(), Bm, Cm), lambda: autograd.block_norm(v, x[:3]),
-                 lambda: autograd.selective_scan(v, step, A, Bm, Cm, h_in=A)):
+                 lambda: autograd.selective_scan(v, step, A, Bm, Cm, h_in=A), lambda: autograd.causal_conv(v, None),
+                 lambda: autograd.selective_scan(v, step, None, Bm, Cm), lambda: autograd.selective_scan(v, None, A, Bm, Cm),
+                 lambda: autograd.selective_scan(v, step, A, None, Cm), lambda: autograd.block_norm(None),
+                 lambda: ops.conv_forward(x, None), lambda: ops.scan_forward(x, step, A, None, Cm),
+                 lambda: ops.norm_backward(None, None, None, None, None, None, None, x)):
         with pytest.raises(ValueError):
             call()
     for call in (lambda: autograd.causal_conv(v, normal(8, 66, 9)), lambda: autograd.block_norm(v, eps=0.0)):
