@@ -195,6 +195,16 @@ inline ScanPlan scan_plan(const snn_scan_cfg* c, int64_t T, int64_t B, int64_t F
     const int64_t want = std::min(std::max<int64_t>(4096 / waves, 2), most);
     if ((waves <= kSplitWaves || groups <= kSplitGroups) && T >= kSplitSteps && want > 1) {
         p.steps = ceil_div(ceil_div(T, want), 16) * 16;      // whole blocks, in either direction
+        if (p.waves == 16) {
+            // One such workgroup fills a CU: the fewest rounds of the 256, weighed with their length
+            // and 16 steps for a segment's start (x[442][2][2928] of 47 states, forward and backward:
+            // 370 us with 5 segments, two rounds, 428 with 3, which are two as well).  8 waves
+            // share a CU in the forward and lose there what the backward gains.
+            const auto cost = [&](int64_t steps) { return ceil_div(groups * ceil_div(T, steps), 256) * (steps + 16); };
+            const int64_t first = p.steps / 32 * 16, last = std::min(2 * p.steps, T - 1);
+            for (int64_t steps = std::max<int64_t>(first, 16); steps <= last; steps += 16)
+                if (ceil_div(T, steps) <= most && cost(steps) < cost(p.steps)) p.steps = steps;
+        }
         p.segments = ceil_div(T, p.steps);
     }
     return p;
