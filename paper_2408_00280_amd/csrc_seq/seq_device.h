@@ -87,21 +87,23 @@ __device__ __forceinline__ float wave_sum(float v) {
     return __uint_as_float(b[0]) + __uint_as_float(b[1]);
 }
 
-// Sums of partial results: a workgroup's 64 values, its waves over the partial results.
+// Sums of partial results: V values of a workgroup, its threads over V values and the partial
+// results, in a fixed order.
+template <int V = kWave>
 __device__ __forceinline__ void reduce_partials(const float* part, int64_t P, int64_t stride, const ReduceOut& out,
-                                                int64_t block, float (*lds)[kWave]) {
-    const int lane = threadIdx.x & (kWave - 1), wave = threadIdx.x / kWave, waves = blockDim.x / kWave;
-    int64_t i = block * kWave + lane;
+                                                int64_t block, float* lds) {
+    const int value = threadIdx.x % V, walker = threadIdx.x / V, walkers = blockDim.x / V;
+    int64_t i = block * V + value;
     const bool in = i < out.n[0] + out.n[1] + out.n[2];
     float s = 0.0f;
     if (in) {
 #pragma unroll 8
-        for (int64_t p = wave; p < P; p += waves) s += part[p * stride + i];
+        for (int64_t p = walker; p < P; p += walkers) s += part[p * stride + i];
     }
-    lds[wave][lane] = s;
+    lds[threadIdx.x] = s;
     __syncthreads();
-    if (wave != 0 || !in) return;
-    for (int w = 1; w < waves; ++w) s += lds[w][lane];
+    if (walker != 0 || !in) return;
+    for (int w = 1; w < walkers; ++w) s += lds[w * V + value];
     int k = 0;
     while (i >= out.n[k]) i -= out.n[k++];
     if (out.p[k] != nullptr) out.p[k][i] = s;

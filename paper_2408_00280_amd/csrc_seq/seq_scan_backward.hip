@@ -271,7 +271,7 @@ constexpr int kJoin = 1024;
 
 template <int IO>
 __global__ __launch_bounds__(kJoin) void scan_join_kernel(ScanArgs a, ReduceOut out, int64_t reduce, int64_t n) {
-    __shared__ float lds[kJoin / kWave][kWave];
+    __shared__ float lds[kJoin];
     if (blockIdx.x < reduce)
         return reduce_partials(a.part_f, a.plan.segments * a.B, scan_partial_values(a.F, a.S), out, blockIdx.x, lds);
     const int64_t i = (blockIdx.x - reduce) * kJoin + threadIdx.x;
