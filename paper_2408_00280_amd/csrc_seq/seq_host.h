@@ -151,9 +151,10 @@ inline snn_status check_scan_cfg(const snn_scan_cfg* c) {
 constexpr int kScanStates = 4;   // states per lane
 constexpr int kScanBlock = 8;    // steps that the waves of the local pass share out at a time
 constexpr int64_t kSplitWaves = 1024, kSplitGroups = 128, kSplitSteps = 128, kMaxSegments = 1024;
-// Up to so many segments a workgroup of the scan walks those before its own itself; a kernel that
-// walks them all first costs a launch more and pays behind that (x[4096][1][1024], 64 segments:
-// 60 us to 60 and the launch; x[1000][8][128], 32: 70 to 77; x[4096][1][512], 128: 55 to 48).
+// Up to so many segments a workgroup of the scan walks those before its own itself (not on a state
+// updated in place: scan_walks); a kernel that walks them all first costs a launch more and pays
+// behind that (x[4096][1][1024], 64 segments: 60 us to 60 and the launch; x[1000][8][128], 32: 70
+// to 77; x[4096][1][512], 128: 55 to 48).
 constexpr int64_t kWalkSegments = 64;
 
 // A workgroup owns 64 features of one group and one sequence, a feature per lane; each of its
@@ -233,9 +234,18 @@ inline int64_t scan_backward_workspace(const snn_scan_cfg* c, int64_t T, int64_t
            piece(p.segments * B * scan_partial_values(F, c->states) * 4);
 }
 
+// Whether the scan's workgroups walk the segments before their own themselves, from the state at
+// `from`.  In place the last segment's workgroup writes the state that the others start from, and
+// nothing orders it behind them: then the carry kernel walks them, which has read the state
+// before the scan starts.  One segment has no others, and its workgroups alone touch their state.
+inline bool scan_walks(const ScanPlan& p, const void* from, const void* to) {
+    return p.segments == 1 || (p.segments <= kWalkSegments && (to == nullptr || to != from));
+}
+
 struct ScanArgs {
     int64_t T, B, F;
     int S, G, softplus;
+    bool walk;       // several segments: the workgroups walk them themselves
     Rows x, dt, Bm, Cm, y, gy, gx, gdt, gB, gC;
     const float *A, *D, *dt_bias, *h_in;
     const int32_t* lengths;

@@ -90,13 +90,13 @@ __device__ __forceinline__ float decayed(float decay, float h) {
     return fabsf(h) < __builtin_inff() ? decay * h : h;
 }
 
-// The state before this segment, or e behind it (DOWN): up to kWalkSegments the workgroup walks
-// the others' states and sums of d itself, more of them the carry kernel has walked.
+// The state before this segment, or e behind it (DOWN): the workgroup walks the others' states and
+// sums of d itself, or the carry kernel has walked them.
 template <bool DOWN>
 __device__ __forceinline__ void segment_state(const ScanArgs& a, const ScanPlace& p, const float (&rate)[kSL],
                                               float (&h)[kSL]) {
     StateColumn states(a, p, a.part_h);
-    if (a.plan.segments > kWalkSegments) {
+    if (!a.walk) {
         if (p.states > 0) states.load(blockIdx.y, h);
         return;
     }

@@ -4,9 +4,11 @@
 // A segment turns the state h before it into (product of its decays) h + (its state from
 // zero), and the product of decays is 2^(A log2 e sum of d): the local kernel forms the state
 // from zero and the sum of d of every segment at once, and the scan then runs on all segments at
-// once, each from its own state.  Where there are few segments its workgroups walk those before
-// their own themselves, else the carry kernel walks them all first.  The backward does the same from the end with e[t] = a[t+1] dL/dh[t+1].  The local pass costs four vector
-// instructions per state and step (20 cycles to the forward's 24) on top of the scan's own.
+// once, each from its own state.  Where there are few segments and the state is not updated in
+// place its workgroups walk those before their own themselves, else the carry kernel walks them
+// all first.  The backward does the same from the end with e[t] = a[t+1] dL/dh[t+1].  The local
+// pass costs four vector instructions per state and step (20 cycles to the forward's 24) on top of
+// the scan's own.
 #include "seq_scan.h"
 
 namespace snnlif {
@@ -164,7 +166,7 @@ snn_status split(const ScanArgs& a, hipStream_t s) {
         case 8: st = local<IO, DOWN, 8>(a, s); break;
         default: st = local<IO, DOWN, 16>(a, s); break;
     }
-    if (st != SNN_OK || a.plan.segments <= kWalkSegments) return st;
+    if (st != SNN_OK || a.walk) return st;
     const int64_t n = a.B * scan_held_states(a.S) * a.F;
     return launch(scan_carry_kernel<DOWN>, grid_for(n), s, a, n);
 }

@@ -207,6 +207,7 @@ snn_status snn_scan_forward(const snn_scan_cfg* cfg, int64_t T, int64_t B, int64
     a.y = rows(y);
     a.h_out = h_out;
     a.saved = static_cast<float*>(saved);
+    a.walk = scan_walks(a.plan, h_in, h_out);
     if (a.plan.segments > 1) {
         int64_t at = 0;
         a.part_h = carve<float>(workspace, at, scan_part_h(cfg, a.plan, B, F));
@@ -245,6 +246,7 @@ snn_status snn_scan_backward(const snn_scan_cfg* cfg, int64_t T, int64_t B, int6
     a.gD = grad_D;
     a.gdt_bias = grad_dt_bias;
     a.gh_in = grad_h_in;
+    a.walk = scan_walks(a.plan, grad_h_out, grad_h_in);
     int64_t at = 0;
     a.part_h = carve<float>(workspace, at, scan_part_h(cfg, a.plan, B, F));
     a.part_d = carve<float>(workspace, at, scan_part_d(a.plan, B, F));
