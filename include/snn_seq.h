@@ -76,7 +76,8 @@ snn_status snn_conv_backward(const snn_conv_cfg *cfg, int64_t T, int64_t B, int6
  * a group,
  *   d[t][b][f]    = softplus(dt[t][b][f] + dt_bias[f])      (or the sum itself)
  *   h[t][b][f][n] = e^{d A[f][n]} h[t-1][b][f][n] + d Bm[t][b][g][n] x[t][b][f]
- *   y[t][b][f]    = sum_n Cm[t][b][g][n] h[t][b][f][n] + D[f] x[t][b][f],   g = f / (F/G). */
+ *   y[t][b][f]    = sum_n Cm[t][b][g][n] h[t][b][f][n] + D[f] x[t][b][f],   g = f / (F/G).
+ * States may grow (d A > 0): each step's e^{d A} has to fit float32, their product need not. */
 typedef struct {
     int32_t io;       /* snn_io: x, dt, Bm, Cm, y and their gradients */
     int32_t states;   /* S, 1 to 64 */

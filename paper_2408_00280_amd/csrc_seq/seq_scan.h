@@ -84,10 +84,14 @@ struct StateColumn {
     }
 };
 
-// A state that is not finite stays so over a segment, as it does step by step, where the decays
-// of a whole segment multiply to 0 in 32 bits.
-__device__ __forceinline__ float decayed(float decay, float h) {
-    return fabsf(h) < __builtin_inff() ? decay * h : h;
+// 2^x h over a segment, x the sum of its steps times the rate.  The decays of a whole segment may
+// multiply to 0 or to infinity in 32 bits where no step's does.  By the whole part of x first, a
+// state that is 0 stays 0 and one that is not finite stays so, as they do step by step, and any
+// other leaves the type only where the product does (2^+-512 takes all of them out of it).
+__device__ __forceinline__ float decayed(float x, float h) {
+    x = __builtin_amdgcn_fmed3f(x, -512.0f, 512.0f);
+    const float whole = floorf(x);
+    return ldexpf(h, int(whole)) * __builtin_amdgcn_exp2f(x - whole);
 }
 
 // The state before this segment, or e behind it (DOWN): the workgroup walks the others' states and
@@ -121,7 +125,7 @@ __device__ __forceinline__ void segment_state(const ScanArgs& a, const ScanPlace
         for (int u = 0; u < U; ++u) {
             if (c0 + u < n) {
 #pragma unroll
-                for (int s = 0; s < kSL; ++s) h[s] = decayed(__builtin_amdgcn_exp2f(d[u] * rate[s]), h[s]) + l[u][s];
+                for (int s = 0; s < kSL; ++s) h[s] = decayed(d[u] * rate[s], h[s]) + l[u][s];
             }
         }
     }

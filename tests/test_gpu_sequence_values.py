@@ -1,0 +1,44 @@
+"""Values at which the scan's sums and products go wrong first: states that grow, infinite inputs
+beside lanes that have none, and what follows the last step of a sequence."""
+import pytest
+import torch
+
+from tests import sequence_ref as R
+from tests.test_gpu_sequence import NAMES, normal
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def ops():
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+    from paper_2408_00280_amd import sequence
+    return sequence
+
+
+def positive(seed, *shape):
+    return normal(seed, *shape).abs() + 0.1
+
+
+@pytest.mark.parametrize("T,B,F,S", [(100, 2, 70, 16), (300, 2, 70, 16), (300, 3, 65, 3), (4096, 1, 20, 4)])
+def test_states_that_grow(ops, T, B, F, S):
+    """Rates above 0 whose growth over a segment of the time axis passes the type: states that are 0
+    until the last steps, and gradients that are 0 but for the first, are finite all the same (in one
+    segment, in some, and in more than a workgroup walks itself).  A step's growth e^x, x < 7.2, is
+    off by 3 roundings of x and 2 of its own, under 24 and with the state's 3 near the 26 per step
+    that R.scan_roundings counts over all T steps, of which at most 8 count here."""
+    g = torch.Generator(device="cuda").manual_seed(1)
+    A = 5 + 1.5 * torch.rand((F, S), device="cuda", generator=g)
+    step = 0.9 + 0.2 * torch.rand((T, B, F), device="cuda", generator=g)
+    x, gy, Bm, Cm = normal(2, T, B, F), normal(3, T, B, F), normal(4, T, B, 1, S), normal(5, T, B, 1, S)
+    x[:T - 8] = 0.0
+    gy[8:] = 0.0
+    ref, mag = (R.scan(x, step, A, Bm, Cm, softplus=False, gy=gy, mag=m) for m in (False, True))
+    h = torch.empty((B, F, S), device="cuda")
+    y, saved = ops.scan_forward(x, step, A, Bm, Cm, softplus=False, h_out=h, train=True)
+    got = ops.scan_backward(x, step, A, Bm, Cm, None, None, saved, gy, softplus=False)
+    n = R.scan_roundings(T, B, F, S)
+    for name, v in zip(("y", "h_out", *NAMES), (y, h, *got)):
+        if v is not None:
+            R.check(name, v, ref[name], mag[name], n)
