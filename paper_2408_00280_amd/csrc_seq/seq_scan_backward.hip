@@ -42,6 +42,48 @@ struct __align__(16) Step {
     float d, dx, gy, x;    // d, d x, dL/dy, x
 };
 
+// Adds one block's part of dL/dA, the first of those that a workgroup goes through, up to the
+// sequence's last step: from memory, each step's state from the block's start.  Hardly a call
+// needs it, so that it takes the kernel's arguments anew rather than hold registers until then.
+template <int IO, int K>
+__device__ void add_block_rates(int t0, float (&gA)[kSL]) {
+    auto args = __builtin_amdgcn_kernarg_segment_ptr();
+    asm volatile("" : "+s"(args));
+    ScanArgs a;
+    __builtin_memcpy(&a, (const void*)args, sizeof(a));
+    const ScanPlace p = scan_place(a);
+    const Columns<IO> cx(a.x, p), cdt(a.dt, p), cgy(a.gy, p);
+    const float bias = a.dt_bias != nullptr ? a.dt_bias[p.f] : 0.0f;
+    float rate[kSL], from[kSL], e[kSL];
+    load_rates(a, p, rate);
+    if (t0 == 0) load_state(a, p, a.h_in, from);
+    else StateColumn(a, p, a.saved).load(t0 / K - 1, from);
+    segment_state<true>(a, p, rate, e);
+#pragma unroll 1
+    for (int t = p.len - 1; t >= t0; --t) {
+        float h[kSL];
+#pragma unroll
+        for (int s = 0; s < kSL; ++s) h[s] = from[s];
+#pragma unroll 1
+        for (int i = t0; i <= t; ++i) {
+            const float v = IoVec<IO, 1>::get(cdt.load(i), 0) + bias, d = a.softplus ? softplus(v) : v;
+            const float dx = d * IoVec<IO, 1>::get(cx.load(i), 0), gy = IoVec<IO, 1>::get(cgy.load(i), 0);
+#pragma unroll
+            for (int s = 0; s < kSL; ++s) {
+                if (s >= p.states) continue;
+                const int64_t n = p.g * a.S + p.first + s;
+                const float dec = __builtin_amdgcn_exp2f(d * rate[s]);
+                if (i < t) {
+                    h[s] = fmaf(dec, h[s], dx * load1<IO>(at<IO>(a.Bm, i, p.b, n)));
+                } else {
+                    e[s] = dec * fmaf(load1<IO>(at<IO>(a.Cm, t, p.b, n)), gy, e[s]);
+                    gA[s] = fmaf(e[s] * h[s], d, gA[s]);
+                }
+            }
+        }
+    }
+}
+
 template <int NS>
 struct BackwardLds {
     static constexpr int K = scan_keep(NS);
@@ -52,8 +94,12 @@ struct BackwardLds {
     float sgbc[K][NS][2 * kSL];  // dL/dB and dL/dC
 };
 
+// Waves per SIMD: 16 waves fill a CU; two of them, with 8-step blocks, are held to the 168 registers
+// of three per SIMD (x[333][5][777]: a pass 73 us, 78 with 169 registers).
+constexpr int backward_waves(int waves) { return waves > 8 ? 4 : waves == 2 ? 3 : 2; }
+
 template <int IO, int NS, bool FULL>
-__global__ __launch_bounds__(NS * kWave, NS > 8 ? 4 : 2) void scan_backward_kernel(ScanArgs a) {
+__global__ __launch_bounds__(NS * kWave, backward_waves(NS)) void scan_backward_kernel(ScanArgs a) {
     constexpr int K = scan_keep(NS), R = K > NS ? K / NS : 1;
     // 4 waves per SIMD need no step read ahead, and have no registers for it
     constexpr bool kAhead = NS <= 8;
@@ -148,7 +194,7 @@ __global__ __launch_bounds__(NS * kWave, NS > 8 ? 4 : 2) void scan_backward_kern
     settle(e);
     settle(h);
     lds_barrier();
-    int buf = 0;
+    int buf = 0, again = -1;
     for (; t0 >= p.t0; t0 -= K) {
         const int below = max(t0 - K, p.t0);
         if (busy) {
@@ -202,6 +248,19 @@ __global__ __launch_bounds__(NS * kWave, NS > 8 ? 4 : 2) void scan_backward_kern
                 if (kAhead) step = ahead;
             }
             sum_up(0);
+            // The steps behind the end have d = 0, and an infinite state or gradient times that is
+            // NaN.  They come first: the sum of their block is formed again at the end, without
+            // them (a branch in each step costs all blocks 7% of their time).
+            if (t0 + K > p.len) {
+                bool nan = false;
+#pragma unroll
+                for (int s = 0; s < kSL; ++s) nan |= gA[s] != gA[s];
+                if (__builtin_amdgcn_ballot_w64(nan) != 0) {
+                    again = t0;
+#pragma unroll
+                    for (int s = 0; s < kSL; ++s) gA[s] = 0.0f;
+                }
+            }
             settle(h_next);      // half a block after their load, and not with the next block's loads
 #pragma unroll
             for (int s = 0; s < kSL; ++s) h[s] = h_next[s];
@@ -248,6 +307,7 @@ __global__ __launch_bounds__(NS * kWave, NS > 8 ? 4 : 2) void scan_backward_kern
         buf ^= 1;
     }
     if (a.gh_in != nullptr && p.t0 == 0) store_state(a, p, a.gh_in, e);
+    if (again >= 0) add_block_rates<IO, K>(again, gA);
     float* pf = a.part_f + (blockIdx.y * a.B + p.b) * scan_partial_values(a.F, a.S);
 #pragma unroll
     for (int i = 0; i < kSL; ++i)

@@ -42,3 +42,29 @@ def test_states_that_grow(ops, T, B, F, S):
     for name, v in zip(("y", "h_out", *NAMES), (y, h, *got)):
         if v is not None:
             R.check(name, v, ref[name], mag[name], n)
+
+
+@pytest.mark.parametrize("S", [3, 16, 33])
+@pytest.mark.parametrize("T,n", [(9, 5), (150, 133), (150, 3)])
+@pytest.mark.parametrize("where", ["x", "gh_out"])
+def test_what_is_infinite_at_a_sequences_end(ops, where, T, n, S):
+    """An infinite input of the last step, or an infinite gradient of the state behind it: the steps
+    that only fill up a block or the batch add nothing to dL/dA.  Held to each sequence alone."""
+    B, F = 2, 67
+    x, dt, Bm, Cm, gy = (positive(i, *s) for i, s in enumerate(((T, B, F), (T, B, F), (T, B, 1, S), (T, B, 1, S), (T, B, F))))
+    A, gh, h, ends = -positive(6, F, S), positive(7, B, F, S), positive(8, B, F, S), [n, T]
+    for b in range(B):
+        if where == "x":
+            x[ends[b] - 1, b, F - 1] = float("inf")
+        else:
+            gh[b, F - 1, S - 1] = float("inf")
+    ln = torch.tensor(ends, dtype=torch.int32, device="cuda")
+    _, saved = ops.scan_forward(x, dt, A, Bm, Cm, h_in=h, lengths=ln, train=True)
+    got = dict(zip(NAMES, ops.scan_backward(x, dt, A, Bm, Cm, None, None, saved, gy, h_in=h, lengths=ln, grad_h_out=gh)))
+    alone = [R.scan(*(v[:m, b:b + 1] for v in (x, dt)), A, *(v[:m, b:b + 1] for v in (Bm, Cm)), h_in=h[b:b + 1],
+                    gy=gy[:m, b:b + 1], gh_out=gh[b:b + 1]) for b, m in enumerate(ends)]
+    pairs = [("gA", got["gA"], alone[0]["gA"] + alone[1]["gA"])]
+    pairs += [(k, got[k][:m, b:b + 1], alone[b][k]) for k in ("gx", "gB", "gC") for b, m in enumerate(ends)]
+    for name, v, ref in pairs:
+        assert torch.equal(torch.isinf(v.cpu()), torch.isinf(ref)), name
+        assert torch.equal(torch.isnan(v.cpu()), torch.isnan(ref)), name
