@@ -89,7 +89,7 @@ struct BackwardLds {
     static constexpr int K = scan_keep(NS);
     Step sd[2][K][kWave];        // this block's, and the next one's as it is staged
     float slope[2][K][kWave];    // of the softplus
-    StagedBC<NS, K> sbc[2];
+    StagedBC<NS, K> sbc[3];      // the last one zeros, for lanes without a feature
     float2 sg[NS][K][kWave];     // (sum dh B, sum dh a h A log2 e)
     float sgbc[K][NS][2 * kSL];  // dL/dB and dL/dC
 };
@@ -108,7 +108,8 @@ __global__ __launch_bounds__(NS * kWave, backward_waves(NS)) void scan_backward_
     const ScanPlace p = scan_place(a);
     float rate[kSL], e[kSL], gA[kSL], gD = 0.0f, gbias = 0.0f;
     load_rates(a, p, rate);
-    // Lanes behind the group's last feature have steps and states of 0 and add nothing.
+    // Lanes behind the group's last feature have steps and states of 0 and add nothing.  Their B
+    // and C are zeros as well: 0 times an infinite one would not be.
     const StateColumn kept(a, p, a.saved);
     const auto load = [&](int64_t c, bool first, float (&v)[kSL]) {
 #pragma unroll
@@ -176,6 +177,7 @@ __global__ __launch_bounds__(NS * kWave, backward_waves(NS)) void scan_backward_
         stage_rows(t0, to);
     };
     fetch(t0);
+    for (int i = threadIdx.x; i < K * NS * 2 * kSL; i += NS * kWave) m.sbc[2].v[0][0][i] = 0.0f;
     stage(t0, 0);
     fetch(t0 - K);
     float h[kSL], h_next[kSL];
@@ -184,7 +186,7 @@ __global__ __launch_bounds__(NS * kWave, backward_waves(NS)) void scan_backward_
         f32x4_t b, c;
     } step, ahead;
     const auto read = [&](int block, int k) {
-        const f32x4_t* bc = reinterpret_cast<const f32x4_t*>(m.sbc[block].v[k][p.wave]);
+        const f32x4_t* bc = reinterpret_cast<const f32x4_t*>(m.sbc[p.active ? block : 2].v[k][p.wave]);
         return Ahead{m.sd[block][k][p.lane], bc[0], bc[1]};
     };
     load(t0 / K - 1, t0 <= 0, h);

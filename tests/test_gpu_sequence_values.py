@@ -68,3 +68,22 @@ def test_what_is_infinite_at_a_sequences_end(ops, where, T, n, S):
     for name, v, ref in pairs:
         assert torch.equal(torch.isinf(v.cpu()), torch.isinf(ref)), name
         assert torch.equal(torch.isnan(v.cpu()), torch.isnan(ref)), name
+
+
+@pytest.mark.parametrize("S", [3, 16])
+@pytest.mark.parametrize("T", [1, 9, 150])
+@pytest.mark.parametrize("which", ["Bm", "Cm"])
+def test_infinite_b_and_c(ops, which, T, S):
+    """An infinite B or C gives infinite results where the definition does: lanes behind the last
+    feature, which see the same B and C, add nothing to the sums over features."""
+    B, F, at = 2, 67, T // 2
+    x, dt, Bm, Cm, gy = (positive(i, *s) for i, s in enumerate(((T, B, F), (T, B, F), (T, B, 1, S), (T, B, 1, S), (T, B, F))))
+    A = -positive(6, F, S)
+    {"Bm": Bm, "Cm": Cm}[which][at, 0, 0, S - 1] = float("inf")
+    h = torch.empty((B, F, S), device="cuda")
+    y, saved = ops.scan_forward(x, dt, A, Bm, Cm, h_out=h, train=True)
+    got = dict(zip(NAMES, ops.scan_backward(x, dt, A, Bm, Cm, None, None, saved, gy)))
+    ref = R.scan(x, dt, A, Bm, Cm, gy=gy)
+    for name, v in {"y": y, "h_out": h, **{k: got[k] for k in ("gx", "gdt", "gA", "gB", "gC")}}.items():
+        assert torch.equal(torch.isinf(v.cpu()), torch.isinf(ref[name])), name
+        assert torch.equal(torch.isnan(v.cpu()), torch.isnan(ref[name])), name
