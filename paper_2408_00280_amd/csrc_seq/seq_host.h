@@ -78,6 +78,16 @@ inline int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
 constexpr int64_t kMaxBlocks = INT32_MAX;
 
+// A launch has fewer than 2^32 threads along x.
+constexpr int64_t kMaxThreads = (int64_t(1) << 32) - 1;
+
+// Workgroups in layers along z, where there are too many for one; those behind the last have
+// nothing to do.  Kernels take blockIdx.z * layer + blockIdx.x, layer being the grid's x.
+inline dim3 layered_grid(int64_t blocks, int threads, int64_t y = 1) {
+    const int64_t layers = ceil_div(blocks, (int64_t(1) << 31) / threads);
+    return dim3(unsigned(ceil_div(blocks, layers)), unsigned(y), unsigned(layers));
+}
+
 // Bytes of a piece of a workspace: pieces start on 256-byte boundaries.
 inline int64_t piece(int64_t bytes) { return (bytes + 255) / 256 * 256; }
 
@@ -258,7 +268,12 @@ struct ScanArgs {
     float* part_h;   // several segments: [segments][B][states][F] and [segments][B][F]
     float* part_d;
     ScanPlan plan;
+    unsigned layer;  // workgroups of a layer of the grid
 };
+// Of the kernels whose workgroups own 64 features each.
+inline dim3 scan_grid(const ScanPlan& p, int64_t B, int64_t G, int64_t segments) {
+    return layered_grid(p.tiles * G * B, p.waves * kWave, segments);
+}
 snn_status scan_split_entry(int io, bool down, const ScanArgs& a, hipStream_t s);
 snn_status scan_forward_entry(int io, const ScanArgs& a, hipStream_t s);
 snn_status scan_backward_entry(int io, const ScanArgs& a, hipStream_t s);

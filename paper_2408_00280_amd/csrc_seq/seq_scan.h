@@ -16,11 +16,17 @@ struct ScanPlace {
     int t0, t1, len;     // the segment, and the steps of the sequence
 };
 
+// The workgroup's number; false behind the last.
+__device__ __forceinline__ unsigned scan_block(const ScanArgs& a) { return blockIdx.z * a.layer + blockIdx.x; }
+__device__ __forceinline__ bool scan_has_block(const ScanArgs& a) {
+    return scan_block(a) < unsigned(a.plan.tiles) * unsigned(a.G) * unsigned(a.B);
+}
+
 __device__ __forceinline__ ScanPlace scan_place(const ScanArgs& a, int first_segment = 0) {
     ScanPlace p;
     p.lane = threadIdx.x & (kWave - 1);
     p.wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
-    const unsigned i = blockIdx.x, tiles = unsigned(a.plan.tiles), per = unsigned(a.F / a.G);
+    const unsigned i = scan_block(a), tiles = unsigned(a.plan.tiles), per = unsigned(a.F / a.G);
     const unsigned q = i / tiles;
     p.tile = i % tiles;
     p.g = q % unsigned(a.G);

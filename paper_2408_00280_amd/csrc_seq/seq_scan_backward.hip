@@ -105,6 +105,7 @@ __global__ __launch_bounds__(NS * kWave, backward_waves(NS)) void scan_backward_
     constexpr bool kAhead = NS <= 8;
     extern __shared__ __align__(16) char lds[];
     auto& m = *reinterpret_cast<BackwardLds<NS>*>(lds);
+    if (!scan_has_block(a)) return;
     const ScanPlace p = scan_place(a);
     float rate[kSL], e[kSL], gA[kSL], gD = 0.0f, gbias = 0.0f;
     load_rates(a, p, rate);
@@ -334,9 +335,10 @@ constexpr int kJoin = 1024;
 template <int IO>
 __global__ __launch_bounds__(kJoin) void scan_join_kernel(ScanArgs a, ReduceOut out, int64_t reduce, int64_t n) {
     __shared__ float lds[kJoin];
-    if (blockIdx.x < reduce)
-        return reduce_partials(a.part_f, a.plan.segments * a.B, scan_partial_values(a.F, a.S), out, blockIdx.x, lds);
-    const int64_t i = (blockIdx.x - reduce) * kJoin + threadIdx.x;
+    const int64_t block = int64_t(blockIdx.z) * a.layer + blockIdx.x;
+    if (block < reduce)
+        return reduce_partials(a.part_f, a.plan.segments * a.B, scan_partial_values(a.F, a.S), out, block, lds);
+    const int64_t i = (block - reduce) * kJoin + threadIdx.x;
     if (i >= n) return;
     const int waves = a.plan.waves, s = int(i % a.S);
     const int64_t q = i / a.S, which = q & 1, r = q >> 1;
@@ -354,7 +356,7 @@ template <int IO, int NS, bool FULL>
 snn_status backward_launch(const ScanArgs& a, hipStream_t s) {
     ScanArgs arg = a;
     void* argv[] = {&arg};
-    const dim3 grid(unsigned(a.plan.tiles * a.G * a.B), unsigned(a.plan.segments));
+    const dim3 grid = scan_grid(a.plan, a.B, a.G, a.plan.segments);
     const hipError_t e = hipLaunchKernel(reinterpret_cast<const void*>(scan_backward_kernel<IO, NS, FULL>), grid,
                                          dim3(NS * kWave), argv, sizeof(BackwardLds<NS>), s);
     return e == hipSuccess ? SNN_OK : SNN_E_LAUNCH;
@@ -377,7 +379,10 @@ snn_status backward_io(const ScanArgs& a, hipStream_t s) {
     if (st != SNN_OK) return st;
     const ReduceOut out = {{a.gA, a.gD, a.gdt_bias}, {a.F * a.S, a.F, a.F}};
     const int64_t reduce = ceil_div(scan_partial_values(a.F, a.S), kWave), n = a.T * a.B * a.G * 2 * a.S;
-    return launch_blk(scan_join_kernel<IO>, dim3(unsigned(reduce + ceil_div(n, kJoin))), kJoin, s, a, out, reduce, n);
+    const dim3 grid = layered_grid(reduce + ceil_div(n, kJoin), kJoin);
+    ScanArgs join = a;
+    join.layer = grid.x;
+    return launch_blk(scan_join_kernel<IO>, grid, kJoin, s, join, out, reduce, n);
 }
 
 }  // namespace

@@ -19,6 +19,7 @@ __global__ __launch_bounds__(NS * kWave) void scan_forward_kernel(ScanArgs a) {
     __shared__ float2 sd[3][K][kWave];           // (d, d x): of this block, the next and the one being staged
     __shared__ float sy[2][NS][K][kWave];
     __shared__ __align__(16) StagedBC<NS, K> sbc[3];
+    if (!scan_has_block(a)) return;
     const ScanPlace p = scan_place(a);
     float rate[kSL], h[kSL];
     load_rates(a, p, rate);
@@ -142,6 +143,7 @@ template <int IO, bool FULL>
 __global__ __launch_bounds__(kWave) void scan_forward_one_kernel(ScanArgs a) {
     constexpr int K = 8;
     __shared__ __align__(16) StagedBC<1, K> sbc[2];
+    if (!scan_has_block(a)) return;
     const ScanPlace p = scan_place(a);
     float rate[kSL], h[kSL];
     load_rates(a, p, rate);
@@ -218,7 +220,7 @@ __global__ __launch_bounds__(kWave) void scan_forward_one_kernel(ScanArgs a) {
 // memory: the states are all but a few percent of what moves.
 template <int IO, int Q, int N>
 __global__ __launch_bounds__(kBlock) void scan_token_kernel(ScanArgs a) {
-    const int64_t i = int64_t(blockIdx.x) * kBlock + threadIdx.x;
+    const int64_t i = (int64_t(blockIdx.z) * a.layer + blockIdx.x) * kBlock + threadIdx.x;
     const unsigned F = unsigned(a.F), B = unsigned(a.B), n = (B + N - 1) / N * F, bf = min(unsigned(i / Q), n - 1);
     const bool active = i / Q < n;               // lanes behind the last feature compute it again
     const unsigned b0 = bf / F * N, f = bf % F, g = f / (F / unsigned(a.G));
@@ -296,12 +298,18 @@ __global__ __launch_bounds__(kBlock) void scan_token_kernel(ScanArgs a) {
     }
 }
 
+template <int IO, int Q, int N>
+snn_status token_sequences(ScanArgs a, hipStream_t s) {
+    const dim3 grid = layered_grid(ceil_div(ceil_div(a.B, N) * a.F * Q, kBlock), kBlock);
+    a.layer = grid.x;
+    return launch(scan_token_kernel<IO, Q, N>, grid, s, a);
+}
+
 template <int IO, int Q>
 snn_status token_lanes(const ScanArgs& a, hipStream_t s) {
     // several sequences per lane where that leaves 16 waves per CU
-    if (a.B * a.F * Q >= int64_t(4) * 256 * 16 * kWave)
-        return launch(scan_token_kernel<IO, Q, 4>, grid_for(ceil_div(a.B, 4) * a.F * Q), s, a);
-    return launch(scan_token_kernel<IO, Q, 1>, grid_for(a.B * a.F * Q), s, a);
+    if (a.B * a.F * Q >= int64_t(4) * 256 * 16 * kWave) return token_sequences<IO, Q, 4>(a, s);
+    return token_sequences<IO, Q, 1>(a, s);
 }
 
 template <int IO>
@@ -317,14 +325,14 @@ snn_status token_states(const ScanArgs& a, hipStream_t s) {
 
 template <int IO, int NS, bool FULL>
 snn_status forward_waves(const ScanArgs& a, hipStream_t s) {
-    const dim3 grid(unsigned(a.plan.tiles * a.G * a.B), unsigned(a.plan.segments));
+    const dim3 grid = scan_grid(a.plan, a.B, a.G, a.plan.segments);
     if constexpr (NS == 1) return launch_blk(scan_forward_one_kernel<IO, FULL>, grid, kWave, s, a);
     // Up to two workgroups of four waves per CU have the LDS for blocks of 16 steps, whose
     // barriers are half as many (x[1024][8][4096]: 208 us to 219 with blocks of 8); more of
     // them hide the barriers themselves and need blocks of 8 to fit (x[4096][1][4096] in 16
     // segments: 89 us to 108 with blocks of 16).
     if constexpr (NS == 4) {
-        if (int64_t(grid.x) * grid.y <= 2 * 256)
+        if (int64_t(grid.x) * grid.y * grid.z <= 2 * 256)
             return launch_blk(scan_forward_kernel<IO, NS, 16, FULL>, grid, NS * kWave, s, a);
     }
     if constexpr (NS > 1) return launch_blk(scan_forward_kernel<IO, NS, 8, FULL>, grid, NS * kWave, s, a);

@@ -21,6 +21,7 @@ __global__ __launch_bounds__(NS * kWave) void scan_local_kernel(ScanArgs a) {
     constexpr int K = kScanBlock, R = K > NS ? K / NS : 1, U = 2;
     __shared__ float2 sd[3][K][kWave];           // (d, d x), or (d, dL/dy)
     __shared__ __align__(16) StagedBC<NS, K> sbc[3];
+    if (!scan_has_block(a)) return;
     // the first segment's state is not needed further down, nor the last one's further up
     const ScanPlace p = scan_place(a, DOWN ? 1 : 0);
     float bias = a.dt_bias != nullptr ? a.dt_bias[p.f] : 0.0f;
@@ -152,7 +153,7 @@ __global__ __launch_bounds__(kBlock) void scan_carry_kernel(ScanArgs a, int64_t 
 
 template <int IO, bool DOWN, int NS>
 snn_status local(const ScanArgs& a, hipStream_t s) {
-    const dim3 grid(unsigned(a.plan.tiles * a.G * a.B), unsigned(a.plan.segments - 1));
+    const dim3 grid = scan_grid(a.plan, a.B, a.G, a.plan.segments - 1);
     return launch_blk(scan_local_kernel<IO, NS, DOWN>, grid, NS * kWave, s, a);
 }
 

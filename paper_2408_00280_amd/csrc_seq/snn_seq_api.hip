@@ -26,7 +26,7 @@ snn_status check_conv(const snn_conv_cfg* c, int64_t T, int64_t B, int64_t F) {
     if (empty(T, B, F)) return SNN_OK;
     for (bool backward : {false, true}) {
         const ConvPlan p = conv_plan(c, T, B, F, backward);
-        if (ceil_div(p.lanes * B * p.chunks, kBlock) > kMaxBlocks) return SNN_E_SHAPE;
+        if (p.lanes * B * p.chunks > kMaxThreads - kBlock) return SNN_E_SHAPE;
     }
     return SNN_OK;
 }
@@ -69,6 +69,7 @@ ScanArgs scan_args(const snn_scan_cfg* c, int64_t T, int64_t B, int64_t F, const
     a.h_in = h_in;
     a.lengths = lengths;
     a.plan = scan_plan(c, T, B, F);
+    a.layer = scan_grid(a.plan, B, a.G, 1).x;
     return a;
 }
 

@@ -4,6 +4,7 @@
 #include <cstdint>
 #include <cstdio>
 #include <initializer_list>
+#include <limits>
 
 #include "seq_host.h"
 
@@ -49,8 +50,61 @@ static void check_states_in_place() {
     CHECK(p.waves == 16 && p.segments > 1 && p.segments <= kWalkSegments && p.tiles * 2 * p.segments > 256);
 }
 
+// Every launch that the checks let through has fewer than 2^32 threads along x and workgroups for
+// all of its work, at the header's limits too.
+static void check_launches() {
+    const auto fits = [](const dim3& g, int64_t blocks, int threads) {
+        return int64_t(g.x) * threads < (int64_t(1) << 32) && g.y <= 65535 && g.z <= 65535 &&
+               int64_t(g.x) * g.z >= blocks && int64_t(g.x) * g.z <= std::numeric_limits<unsigned>::max() &&
+               int64_t(g.x) * (g.z - 1) < blocks;
+    };
+    for (int threads : {64, 128, 256, 512, 1024})
+        for (int64_t blocks : {int64_t(1), int64_t(2), int64_t(255), (int64_t(1) << 21) - 1, int64_t(1) << 21,
+                               (int64_t(1) << 21) + 1, (int64_t(1) << 26) + 7, kMaxBlocks - 1, kMaxBlocks}) {
+            const dim3 g = layered_grid(blocks, threads);
+            CHECK(fits(g, blocks, threads));
+            if (blocks * threads <= int64_t(1) << 31) CHECK(g.z == 1 && g.x == blocks);
+        }
+    const int64_t K = 1024, M = K * K;
+    struct Shape {
+        int64_t T, B, F;
+        int G;
+    };
+    for (const Shape& s : {Shape{4096, 1024, 512, 8}, {64, 65536, 8, 8}, {2, 16384, 4096, 4096}, {2, 65536, 4096, 1},
+                           {1, 16384, 65536, 1}, {1, 128, 16 * M, 1}, {1, 1, 16 * M, 16 * int(M)}, {K * M, 1, 1, 1},
+                           {1, 16 * M, 128, 1}, {32, 16 * M, 2, 2}})
+        for (int S : {1, 4, 16, 64}) {
+            const snn_scan_cfg c = {SNN_IO_BF16, S, s.G, 1};
+            CHECK(check_seq_shape(s.T, s.B, s.F) == SNN_OK);
+            const ScanPlan p = scan_plan(&c, s.T, s.B, s.F);
+            const int64_t blocks = p.tiles * s.G * s.B;
+            CHECK(blocks <= kMaxBlocks && s.T * s.B * s.G <= kMaxBlocks);
+            CHECK(fits(scan_grid(p, s.B, s.G, p.segments), blocks, p.waves * kWave));
+            const int64_t join = ceil_div(scan_partial_values(s.F, S), kWave) + ceil_div(s.T * s.B * s.G * 2 * S, 1024);
+            CHECK(fits(layered_grid(join, 1024), join, 1024));
+            for (int n : {1, 4}) {
+                const int64_t token = ceil_div(ceil_div(s.B, n) * s.F * p.waves, 256);
+                CHECK(fits(layered_grid(token, 256), token, 256));
+            }
+            if (p.segments > 1) CHECK(s.B * scan_held_states(S) * s.F <= kMaxThreads - kBlock);
+        }
+    // the convolution's lanes up to B * F = 2^31, and the sums of partial results
+    for (const Shape& s : {Shape{1, 128, 16 * M, 1}, {32, 16 * M, 128, 1}, {K * M, 1, 1, 1}, {64, 16 * M, 16, 1}, {1, 16 * M, 127, 1}})
+        for (bool backward : {false, true}) {
+            const snn_conv_cfg c = {SNN_IO_F32, 8, SNN_ACT_SILU};
+            const ConvPlan p = conv_plan(&c, s.T, s.B, s.F, backward);
+            CHECK(p.lanes * s.B * p.chunks <= kMaxThreads - kBlock);
+        }
+    const snn_conv_cfg widest = {SNN_IO_F32, kMaxTaps, SNN_ACT_SILU};
+    CHECK(ceil_div(conv_partial(&widest, kMaxSeqF), kWave) * 1024 <= kMaxThreads);
+    CHECK(ceil_div(3 * kMaxSeqF, kWave) * 1024 <= kMaxThreads);
+    // the example that a grid of one layer does not take
+    CHECK(layered_grid(ceil_div(int64_t(4096) * 1024 * 8 * 2 * 64, 1024), 1024).z > 1);
+}
+
 int main() {
     check_states_in_place();
+    check_launches();
     if (failures != 0) return 1;
     std::puts("all checks passed");
     return 0;

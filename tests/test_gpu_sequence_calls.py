@@ -1,9 +1,9 @@
 """Calls of the sequence operators that their documentation allows and that go wrong first: states
-updated in place over many workgroups."""
+updated in place over many workgroups, launches of more threads than a grid takes."""
 import pytest
 import torch
 
-from tests.test_gpu_sequence import lengths_of, scan_inputs
+from tests.test_gpu_sequence import lengths_of, normal, scan_inputs
 
 pytestmark = pytest.mark.gpu
 
@@ -31,3 +31,39 @@ def test_scan_states_in_place(ops, T, B, F, S, io, ragged):
         state = h.clone()
         got, _ = ops.scan_forward(x, step, A, Bm, Cm, D, bias, h_in=state, h_out=state, lengths=ln)
         assert torch.equal(got, y) and torch.equal(state, out)
+
+
+def of_sequences(rows, at):
+    return [v[:, at].contiguous() for v in rows]
+
+
+@pytest.mark.parametrize("T,B,F,S,G", [(2, 16384, 4096, 1, 4096), (64, 65536, 8, 64, 8)])
+def test_launches_of_more_than_a_grids_threads(ops, T, B, F, S, G):
+    """More workgroups, and more sums of partial results, than 2^32 threads of one grid axis: some
+    sequences by themselves give the same bits."""
+    x, step, gy = (normal(i, T, B, F, dtype=torch.bfloat16) for i in (1, 2, 3))
+    Bm, Cm = (normal(i, T, B, G, S, dtype=torch.bfloat16) for i in (4, 5))
+    A, D, bias = -torch.exp(normal(6, F, S, sd=0.7)), normal(7, F), normal(8, F, mean=-1.0)
+    at = torch.tensor([0, 1, B // 2 - 1, B // 2, B - 2, B - 1], device="cuda")
+    part = of_sequences((x, step, Bm, Cm, gy), at)
+
+    def run(x, step, Bm, Cm, gy):
+        y, saved = ops.scan_forward(x, step, A, Bm, Cm, D, bias, train=True)
+        g = ops.scan_backward(x, step, A, Bm, Cm, D, bias, saved, gy)
+        return [y, g[0], g[1], g[3], g[4]], [g[2], g[5], g[6]]
+    rows, params = run(x, step, Bm, Cm, gy)
+    for v, w in zip(of_sequences(rows, at), run(*part)[0]):
+        assert torch.equal(v, w)
+    assert all(torch.isfinite(v).all() for v in params)
+
+
+def test_tokens_of_more_than_a_grids_threads(ops):
+    """One step of 2^30 features of 64 states, 16 lanes each for 4 sequences."""
+    B, F, S = 16384, 65536, 64
+    x = normal(1, 1, B, F, dtype=torch.bfloat16)
+    Bm, Cm = (normal(i, 1, B, 1, S, dtype=torch.bfloat16) for i in (2, 3))
+    A = -torch.exp(normal(4, F, S, sd=0.7))
+    y, _ = ops.scan_forward(x, x, A, Bm, Cm)
+    at = torch.tensor([0, 1, B // 2 - 1, B // 2, B - 2, B - 1], device="cuda")
+    part = of_sequences((x, Bm, Cm), at)
+    assert torch.equal(y[:, at], ops.scan_forward(part[0], part[0], A, *part[1:])[0])
