@@ -336,9 +336,13 @@ variable_list once(variable_list grads, size_t others) {
     return grads;
 }
 
-bool any_requires_grad(std::initializer_list<Tensor> all) {
-    if (!at::GradMode::is_enabled()) return false;
-    return std::any_of(all.begin(), all.end(), [](const Tensor& a) { return a.defined() && a.requires_grad(); });
+// Whether autograd has to hear of a call: a gradient is wanted, or an input has a forward-mode
+// tangent, which the functions below have no rule for and refuse.
+bool differentiated(std::initializer_list<Tensor> all) {
+    const bool grad = at::GradMode::is_enabled();
+    return std::any_of(all.begin(), all.end(), [grad](const Tensor& a) {
+        return a.defined() && ((grad && a.requires_grad()) || a._fw_grad(/*level=*/0).defined());
+    });
 }
 
 Tensor zeros_if_none(const Tensor& g, const Tensor& x) { return g.defined() ? g : at::zeros_like(x); }
@@ -367,7 +371,7 @@ variable_list causal_conv(const Tensor& x, const Tensor& weight, const Optional&
                           const Optional& lengths, bool want_state) {
     io_of(x);
     if (!weight.defined() || weight.dim() != 2 || weight.size(1) < 1) refuse("weight must be [F, W], act None or 'silu'");
-    if (any_requires_grad({x, weight, or_none(bias), or_none(state)}))
+    if (differentiated({x, weight, or_none(bias), or_none(state)}))
         return Conv::apply(x, weight, bias, state, lengths, act, want_state);
     Tensor out;
     if (want_state) out = at::empty({weight.size(1) - 1, x.size(1), x.size(2)}, x.options());
@@ -402,7 +406,7 @@ variable_list selective_scan(const Tensor& x, const Tensor& dt, const Tensor& A,
     io_of(x);
     if (!dt.defined() || !A.defined() || A.dim() != 2 || !Bm.defined() || !Cm.defined())
         refuse("dt must be [T, B, F], A [F, S], Bm and Cm [T, B, G, S]");
-    if (any_requires_grad({x, dt, A, Bm, Cm, or_none(D), or_none(dt_bias), or_none(h_in)}))
+    if (differentiated({x, dt, A, Bm, Cm, or_none(D), or_none(dt_bias), or_none(h_in)}))
         return Scan::apply(x, dt, A, Bm, Cm, D, dt_bias, h_in, lengths, softplus, want_state);
     Tensor out;
     if (want_state) out = at::empty({x.size(1), A.size(0), A.size(1)}, x.options().dtype(at::kFloat));
@@ -432,7 +436,7 @@ struct Norm : torch::autograd::Function<Norm> {
 
 variable_list block_norm(const Tensor& y, const Optional& r, const Optional& z, const Optional& w_post,
                          const Optional& scale, const Optional& w_pre, const Optional& lengths, double eps) {
-    if (any_requires_grad({y, or_none(r), or_none(z), or_none(w_post), or_none(scale), or_none(w_pre)}))
+    if (differentiated({y, or_none(r), or_none(z), or_none(w_post), or_none(scale), or_none(w_pre)}))
         return Norm::apply(y, r, z, w_post, scale, w_pre, lengths, eps);
     return norm_forward(y, or_none(r), or_none(z), or_none(w_post), or_none(scale), or_none(w_pre), eps, or_none(lengths),
                         false);

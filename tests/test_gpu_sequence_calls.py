@@ -67,3 +67,26 @@ def test_tokens_of_more_than_a_grids_threads(ops):
     at = torch.tensor([0, 1, B // 2 - 1, B // 2, B - 2, B - 1], device="cuda")
     part = of_sequences((x, Bm, Cm), at)
     assert torch.equal(y[:, at], ops.scan_forward(part[0], part[0], A, *part[1:])[0])
+
+
+def test_tangents_are_refused(ops):
+    """Forward-mode derivatives have no rule here: a tangent on any input raises an error instead of
+    coming out as none, with gradients wanted and without."""
+    import torch.autograd.forward_ad as fw
+
+    from paper_2408_00280_amd import autograd
+    x, step, A, Bm, Cm, D, *_ = scan_inputs("f32", 5, 2, 66, 4, 1, "D")
+    w = normal(9, 66, 4)
+    calls = {"conv x": (autograd.causal_conv, [x, w], 0), "conv weight": (autograd.causal_conv, [x, w], 1),
+             "scan x": (autograd.selective_scan, [x, step, A, Bm, Cm], 0),
+             "scan C": (autograd.selective_scan, [x, step, A, Bm, Cm], 4),
+             "scan D": (autograd.selective_scan, [x, step, A, Bm, Cm, D], 5),
+             "norm y": (autograd.block_norm, [x, step], 0), "norm r": (autograd.block_norm, [x, step], 1)}
+    for name, (fn, args, at) in calls.items():
+        with fw.dual_level():
+            dual = [fw.make_dual(v, torch.ones_like(v)) if i == at else v for i, v in enumerate(args)]
+            for grad in (True, False):
+                with torch.set_grad_enabled(grad), pytest.raises(RuntimeError, match="jvp"):
+                    fn(*dual)
+                    raise AssertionError(f"{name}: the tangent was dropped")
+        fn(*args)
