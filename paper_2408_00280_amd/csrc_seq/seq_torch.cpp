@@ -6,6 +6,7 @@
 // 10 us on the GPU, and what stood here in Python before took 10 to 15 us per call and, in a
 // backward, which runs on a thread of its own, 45 to 120 us.
 #include <ATen/Functions.h>
+#include <ATen/TracerMode.h>
 #include <c10/core/DeviceGuard.h>
 #include <c10/hip/HIPStream.h>
 #include <torch/csrc/autograd/custom_function.h>
@@ -468,6 +469,9 @@ auto bound(R (*fn)(A...)) {
         R out;
         {
             const py::gil_scoped_release free;
+            // a trace would record where the outputs are allocated and not what fills them
+            if (at::tracer::impl::is_dispatch_enabled())
+                throw std::runtime_error("the sequence operators cannot be traced by torch.jit.trace");
             out = fn(FromPython<A>::pass(a)...);
         }
         return to_python(out);

@@ -90,3 +90,17 @@ def test_tangents_are_refused(ops):
                     fn(*dual)
                     raise AssertionError(f"{name}: the tangent was dropped")
         fn(*args)
+
+
+def test_traces_are_refused(ops):
+    """A tracer would keep the outputs' allocation and none of the work."""
+    from paper_2408_00280_amd import autograd
+    x, step, A, Bm, Cm, *_ = scan_inputs("f32", 5, 2, 66, 4, 1, "")
+    w = normal(9, 66, 4)
+    for fn in (lambda v: autograd.causal_conv(v, w), lambda v: autograd.selective_scan(v, step, A, Bm, Cm),
+               lambda v: autograd.block_norm(v)[0], lambda v: ops.conv_forward(v, w), lambda v: ops.norm_forward(v)[0],
+               lambda v: ops.scan_forward(v, step, A, Bm, Cm)[0]):
+        for grad in (False, True):
+            with pytest.raises(RuntimeError, match="trace"):
+                torch.jit.trace(fn, x.clone().requires_grad_(grad), check_trace=False)
+                raise AssertionError("was traced")
