@@ -16,12 +16,12 @@ BlockNorm.
 """
 from __future__ import annotations
 
+import functools
 import math
 
 import torch
 
-from . import layer, sequence
-from .sequence import _sequence
+from . import layer
 
 _IO = {torch.float32: "f32", torch.bfloat16: "bf16"}
 
@@ -177,10 +177,18 @@ class LIFStack(torch.nn.Module):
                 f"v_th={self.v_th}, v_reset={self.v_reset}, alpha={self.alpha}, reset={self.reset}")
 
 
+@functools.cache
+def _ops():
+    """The sequence operators, at their first use: the LIF layers do without their module."""
+    from . import sequence
+    return sequence
+
+
 def causal_conv(x, weight, bias=None, *, act="silu", state=None, lengths=None, return_state=False):
     """Short causal convolution of x[T, B, F] along time (see sequence.conv_forward), with
     gradients for x, weight, bias and state.  Returns y, or (y, the last W-1 inputs)."""
-    out = _sequence.causal_conv(x, weight, bias, sequence.act_code(act), state, lengths, return_state)
+    ops = _ops()
+    out = ops._sequence.causal_conv(x, weight, bias, ops.act_code(act), state, lengths, return_state)
     return out if return_state else out[0]
 
 
@@ -204,7 +212,7 @@ class CausalConv(torch.nn.Module):
     @torch.no_grad()
     def step(self, x, state):
         """One step x[B, F] on state[W-1, B, F], which is updated in place: y[B, F]."""
-        return sequence.conv_forward(x[None], *self._args(), act=self.act, state=state, state_out=state)[0]
+        return _ops().conv_forward(x[None], *self._args(), act=self.act, state=state, state_out=state)[0]
 
     def extra_repr(self) -> str:
         return f"features={self.weight.shape[0]}, width={self.weight.shape[1]}, act={self.act}"
@@ -214,7 +222,7 @@ def selective_scan(x, dt, A, Bm, Cm, D=None, dt_bias=None, *, softplus=True, h_i
                    return_state=False):
     """Selective state space scan of x[T, B, F] (see sequence.scan_forward), with gradients for
     every input.  Returns y, or (y, the state [B, F, S] after the last step)."""
-    out = _sequence.selective_scan(x, dt, A, Bm, Cm, D, dt_bias, bool(softplus), h_in, lengths, return_state)
+    out = _ops()._sequence.selective_scan(x, dt, A, Bm, Cm, D, dt_bias, bool(softplus), h_in, lengths, return_state)
     return out if return_state else out[0]
 
 
@@ -242,8 +250,8 @@ class SelectiveScan(torch.nn.Module):
     def step(self, x, dt, Bm, Cm, h):
         """One step x, dt [B, F], Bm, Cm [B, G, S] on the state h[B, F, S], which is updated in
         place: y[B, F]."""
-        y, _ = sequence.scan_forward(x[None], dt[None], self._A(), Bm[None], Cm[None], self.D.float(),
-                                     self.dt_bias.float(), h_in=h, h_out=h)
+        y, _ = _ops().scan_forward(x[None], dt[None], self._A(), Bm[None], Cm[None], self.D.float(),
+                                   self.dt_bias.float(), h_in=h, h_out=h)
         return y[0]
 
     def extra_repr(self) -> str:
@@ -253,7 +261,7 @@ class SelectiveScan(torch.nn.Module):
 def block_norm(y, r=None, z=None, w_post=None, scale=None, w_pre=None, *, eps=1e-5, lengths=None):
     """A block's gate, norm and scaled residual with the next block's norm (see
     sequence.norm_forward), with gradients for every input: (r_new, u or None)."""
-    out = _sequence.block_norm(y, r, z, w_post, scale, w_pre, lengths, eps)
+    out = _ops()._sequence.block_norm(y, r, z, w_post, scale, w_pre, lengths, eps)
     return out[0], out[1] if w_pre is not None else None
 
 
