@@ -45,15 +45,22 @@ int io_of(const Tensor& x) {
     return x.scalar_type() == at::kFloat ? SNN_IO_F32 : SNN_IO_BF16;
 }
 
-// `a` with the axes behind the second contiguous.
-Tensor rows(const Tensor& a) {
-    if (a.is_contiguous()) return a;
+// Whether the axes behind the second are contiguous.
+bool has_rows(const Tensor& a) {
     int64_t n = 1;
     for (int64_t d = a.dim() - 1; d >= 2; --d) {
-        if (a.size(d) != 1 && a.stride(d) != n) return a.contiguous();
+        if (a.size(d) != 1 && a.stride(d) != n) return false;
         n *= a.size(d);
     }
-    return a;
+    return true;
+}
+Tensor rows(const Tensor& a) { return a.is_contiguous() || has_rows(a) ? a : a.contiguous(); }
+
+// An output shaped like the rows of `a`, in its order of steps and sequences.  Where rows of `a`
+// overlap that order may put an axis inside the rows: then dense and time-major.
+Tensor rows_like(const Tensor& a) {
+    Tensor out = at::empty_like(a);
+    return out.is_contiguous() || has_rows(out) ? out : at::empty(a.sizes(), a.options());
 }
 
 void check_tensor(const char* name, const Tensor& a, const Tensor& x, at::IntArrayRef shape, at::ScalarType dtype,
@@ -97,7 +104,7 @@ Tensor bytes(size_t n, const Tensor& x) {
     return n == 0 ? Tensor() : at::empty({int64_t(n)}, x.options().dtype(at::kByte));
 }
 
-Tensor like(const Tensor& a) { return a.defined() ? at::empty_like(a) : a; }
+Tensor like(const Tensor& a) { return a.defined() ? rows_like(a) : a; }
 
 // A parameter's gradient: the kernels write it whole, unless there is nothing to do.
 Tensor param_like(const Tensor& p, bool empty) {
@@ -150,7 +157,7 @@ Tensor conv_forward(const Tensor& x, const Tensor& weight, const Tensor& bias, i
     const ConvCall c(x, weight, bias, act, state, lengths);
     const c10::DeviceGuard guard(x.device());
     void* out = c.state_like("state_out", state_out);
-    Tensor y = at::empty_like(c.x);
+    Tensor y = rows_like(c.x);
     if (c.empty()) hand_over(state_out, state);
     else
         check("snn_conv_forward", snn_conv_forward(&c.cfg, c.T, c.B, c.F, Seq(c.x), c.weight, c.bias, c.state, c.lengths,
@@ -165,7 +172,7 @@ variable_list conv_backward(const Tensor& x, const Tensor& weight, const Tensor&
     const c10::DeviceGuard guard(x.device());
     const Tensor gy = data("grad_y", grad_y, c.x, {c.T, c.B, c.F});
     const void* g_out = c.state_like("grad_state_out", grad_state_out);
-    Tensor gx = at::empty_like(c.x), gw = param_like(weight, c.empty()), gb = param_like(bias, c.empty()), gs = like(state);
+    Tensor gx = rows_like(c.x), gw = param_like(weight, c.empty()), gb = param_like(bias, c.empty()), gs = like(state);
     if (c.empty()) {
         hand_over(gs, grad_state_out);
     } else {
@@ -217,7 +224,7 @@ variable_list scan_forward(const Tensor& x, const Tensor& dt, const Tensor& A, c
     const c10::DeviceGuard guard(x.device());
     float* out = dense("h_out", h_out, c.x, {c.B, c.F, c.S});
     if (train && out != nullptr && out == c.h_in) refuse("the backward reads h_in: h_out must be another tensor");
-    Tensor y = at::empty_like(c.x), saved;
+    Tensor y = rows_like(c.x), saved;
     if (train) saved = at::empty({int64_t(c.saved)}, x.options().dtype(at::kByte));
     if (c.empty()) {
         hand_over(h_out, h_in);
@@ -241,7 +248,7 @@ variable_list scan_backward(const Tensor& x, const Tensor& dt, const Tensor& A, 
     const Tensor gy = data("grad_y", grad_y, c.x, {c.T, c.B, c.F});
     const float* g_out = dense("grad_h_out", grad_h_out, c.x, {c.B, c.F, c.S});
     const bool none = c.empty();
-    Tensor gx = at::empty_like(c.x), gdt = at::empty_like(c.x), gB = at::empty_like(c.Bm), gC = at::empty_like(c.Cm);
+    Tensor gx = rows_like(c.x), gdt = rows_like(c.x), gB = rows_like(c.Bm), gC = rows_like(c.Cm);
     Tensor gA = param_like(A, none), gD = param_like(D, none), gbias = param_like(dt_bias, none), gh = like(h_in);
     if (none) {
         gB.zero_();
@@ -286,8 +293,8 @@ variable_list norm_forward(const Tensor& y, const Tensor& r, const Tensor& z, co
                            const Tensor& w_pre, double eps, const Tensor& lengths, bool train) {
     const NormCall c(y, r, z, w_post, scale, w_pre, eps, lengths);
     const c10::DeviceGuard guard(y.device());
-    Tensor r_new = at::empty_like(c.y), u, rstd;
-    if (w_pre.defined()) u = at::empty_like(c.y);
+    Tensor r_new = rows_like(c.y), u, rstd;
+    if (w_pre.defined()) u = rows_like(c.y);
     if (train) rstd = at::empty({2, c.T, c.B}, y.options().dtype(at::kFloat));
     if (!c.empty())
         check("snn_norm_forward",

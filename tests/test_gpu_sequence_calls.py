@@ -1,5 +1,6 @@
 """Calls of the sequence operators that their documentation allows and that go wrong first: states
-updated in place over many workgroups, launches of more threads than a grid takes."""
+updated in place over many workgroups, launches of more threads than a grid takes,
+tangents and traces, rows that overlap."""
 import pytest
 import torch
 
@@ -104,3 +105,25 @@ def test_traces_are_refused(ops):
             with pytest.raises(RuntimeError, match="trace"):
                 torch.jit.trace(fn, x.clone().requires_grad_(grad), check_trace=False)
                 raise AssertionError("was traced")
+
+
+@pytest.mark.parametrize("steps", [(1, 40), (40, 1), (2, 40)])
+def test_windows_that_overlap(ops, steps):
+    """Rows that share elements with the next, a step of 1 apart: the same as their copies."""
+    T, B, F, S, W = 6, 3, 8, 4, 4
+    room = normal(1, 1000)
+    x = room.as_strided((T, B, F), (*steps, 1))
+    bc = room[200:].as_strided((T, B, 2, S), (*steps, S, 1))
+    A, w, one, gy = -positive_rates(F, S), normal(3, F, W), normal(4, F), normal(5, T, B, F)
+
+    def run(x, bc):
+        y, saved = ops.scan_forward(x, x, A, bc, bc, train=True)
+        r, u, rstd = ops.norm_forward(x, x, x, one, one, one, train=True)
+        return [y, *ops.scan_backward(x, x, A, bc, bc, None, None, saved, gy)[:5], ops.conv_forward(x, w),
+                *ops.conv_backward(x, w, None, gy)[:2], r, u, *ops.norm_backward(x, x, x, one, one, one, rstd, gy, x)]
+    for a, b in zip(run(x, bc), run(x.contiguous(), bc.contiguous())):
+        assert torch.equal(a, b)
+
+
+def positive_rates(F, S):
+    return normal(2, F, S).abs() + 0.1
