@@ -212,36 +212,52 @@ inline ScanPlan scan_plan(const snn_scan_cfg* c, int64_t T, int64_t B, int64_t F
             // 370 us with 5 segments, two rounds, 428 with 3, which are two as well).  8 waves
             // share a CU in the forward and lose there what the backward gains.
             const auto cost = [&](int64_t steps) { return ceil_div(groups * ceil_div(T, steps), 256) * (steps + 16); };
-            const int64_t first = p.steps / 32 * 16, last = std::min(2 * p.steps, T - 1);
-            for (int64_t steps = std::max<int64_t>(first, 16); steps <= last; steps += 16)
-                if (ceil_div(T, steps) <= most && cost(steps) < cost(p.steps)) p.steps = steps;
+            // Half to twice the length; of as many segments the shortest are the cheapest.
+            const auto blocks = [](int64_t steps) { return ceil_div(steps, 16) * 16; };
+            const int64_t last = std::min(2 * p.steps, T - 1);
+            int64_t steps = std::max({p.steps / 32 * 16, blocks(ceil_div(T, most)), int64_t(16)}), least = cost(p.steps);
+            while (steps <= last) {
+                if (const int64_t now = cost(steps); now < least) {
+                    least = now;
+                    p.steps = steps;
+                }
+                const int64_t n = ceil_div(T, steps);       // 2 at least, as steps < T
+                steps = std::max(steps + 16, blocks(ceil_div(T, n - 1)));
+            }
         }
         p.segments = ceil_div(T, p.steps);
     }
     return p;
 }
 
+inline int64_t scan_saved(const snn_scan_cfg* c, const ScanPlan& p, int64_t T, int64_t B, int64_t F) {
+    return (ceil_div(T, p.keep) - 1) * B * F * scan_held_states(c->states) * 4;
+}
 inline int64_t scan_saved(const snn_scan_cfg* c, int64_t T, int64_t B, int64_t F) {
-    return (ceil_div(T, scan_plan(c, T, B, F).keep) - 1) * B * F * scan_held_states(c->states) * 4;
+    return scan_saved(c, scan_plan(c, T, B, F), T, B, F);
 }
 // The segments' states and their sums of d.
 inline int64_t scan_part_h(const snn_scan_cfg* c, const ScanPlan& p, int64_t B, int64_t F) {
     return p.segments > 1 ? p.segments * B * F * scan_held_states(c->states) * 4 : 0;
 }
 inline int64_t scan_part_d(const ScanPlan& p, int64_t B, int64_t F) { return p.segments > 1 ? p.segments * B * F * 4 : 0; }
-inline int64_t scan_forward_workspace(const snn_scan_cfg* c, int64_t T, int64_t B, int64_t F) {
-    const ScanPlan p = scan_plan(c, T, B, F);
+inline int64_t scan_forward_workspace(const snn_scan_cfg* c, const ScanPlan& p, int64_t B, int64_t F) {
     return piece(scan_part_h(c, p, B, F)) + piece(scan_part_d(p, B, F));
+}
+inline int64_t scan_forward_workspace(const snn_scan_cfg* c, int64_t T, int64_t B, int64_t F) {
+    return scan_forward_workspace(c, scan_plan(c, T, B, F), B, F);
 }
 constexpr int64_t scan_partial_values(int64_t F, int S) { return F * (S + 2); }
 // dL/dB and dL/dC of every tile, as the waves hold them.
 inline int64_t scan_partial_bc(const snn_scan_cfg* c, const ScanPlan& p, int64_t T, int64_t B) {
     return p.tiles * T * B * c->groups * p.waves * 2 * kScanStates * 4;
 }
-inline int64_t scan_backward_workspace(const snn_scan_cfg* c, int64_t T, int64_t B, int64_t F) {
-    const ScanPlan p = scan_plan(c, T, B, F);
+inline int64_t scan_backward_workspace(const snn_scan_cfg* c, const ScanPlan& p, int64_t T, int64_t B, int64_t F) {
     return piece(scan_part_h(c, p, B, F)) + piece(scan_part_d(p, B, F)) + piece(scan_partial_bc(c, p, T, B)) +
            piece(p.segments * B * scan_partial_values(F, c->states) * 4);
+}
+inline int64_t scan_backward_workspace(const snn_scan_cfg* c, int64_t T, int64_t B, int64_t F) {
+    return scan_backward_workspace(c, scan_plan(c, T, B, F), T, B, F);
 }
 
 // Whether the scan's workgroups walk the segments before their own themselves, from the state at

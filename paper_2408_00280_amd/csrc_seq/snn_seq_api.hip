@@ -31,13 +31,14 @@ snn_status check_conv(const snn_conv_cfg* c, int64_t T, int64_t B, int64_t F) {
     return SNN_OK;
 }
 
-snn_status check_scan(const snn_scan_cfg* c, int64_t T, int64_t B, int64_t F) {
+// With the plan, where there is anything to do.
+snn_status check_scan(const snn_scan_cfg* c, int64_t T, int64_t B, int64_t F, ScanPlan& p) {
     const snn_status st = check_scan_cfg(c);
     if (st != SNN_OK) return st;
     if (check_seq_shape(T, B, F) != SNN_OK) return SNN_E_SHAPE;
     if (F % c->groups != 0) return SNN_E_SHAPE;
     if (empty(T, B, F)) return SNN_OK;
-    const ScanPlan p = scan_plan(c, T, B, F);
+    p = scan_plan(c, T, B, F);
     if (p.tiles * c->groups > kMaxBlocks / B || F > kMaxN / B) return SNN_E_SHAPE;
     return T * B * c->groups <= kMaxBlocks && F * c->states <= kMaxSpan / B ? SNN_OK : SNN_E_SHAPE;
 }
@@ -49,7 +50,7 @@ snn_status check_norm(const snn_norm_cfg* c, int64_t T, int64_t B, int64_t F) {
     return SNN_OK;
 }
 
-ScanArgs scan_args(const snn_scan_cfg* c, int64_t T, int64_t B, int64_t F, const snn_seq* x, const snn_seq* dt,
+ScanArgs scan_args(const snn_scan_cfg* c, const ScanPlan& plan, int64_t T, int64_t B, int64_t F, const snn_seq* x, const snn_seq* dt,
                    const float* A, const snn_seq* Bm, const snn_seq* Cm, const float* D, const float* dt_bias,
                    const float* h_in, const int32_t* lengths) {
     ScanArgs a = {};
@@ -68,7 +69,7 @@ ScanArgs scan_args(const snn_scan_cfg* c, int64_t T, int64_t B, int64_t F, const
     a.dt_bias = dt_bias;
     a.h_in = h_in;
     a.lengths = lengths;
-    a.plan = scan_plan(c, T, B, F);
+    a.plan = plan;
     a.layer = scan_grid(a.plan, B, a.G, 1).x;
     return a;
 }
@@ -177,20 +178,22 @@ snn_status snn_conv_backward(const snn_conv_cfg* cfg, int64_t T, int64_t B, int6
 }
 
 snn_status snn_scan_saved_bytes(const snn_scan_cfg* cfg, int64_t T, int64_t B, int64_t F, size_t* bytes) {
-    const snn_status st = check_scan(cfg, T, B, F);
+    ScanPlan plan;
+    const snn_status st = check_scan(cfg, T, B, F, plan);
     if (st != SNN_OK) return st;
     if (bytes == nullptr) return SNN_E_NULL;
-    *bytes = empty(T, B, F) ? 0 : size_t(scan_saved(cfg, T, B, F));
+    *bytes = empty(T, B, F) ? 0 : size_t(scan_saved(cfg, plan, T, B, F));
     return SNN_OK;
 }
 
 snn_status snn_scan_workspace_bytes(const snn_scan_cfg* cfg, int64_t T, int64_t B, int64_t F, size_t* forward_bytes,
                                     size_t* backward_bytes) {
-    const snn_status st = check_scan(cfg, T, B, F);
+    ScanPlan plan;
+    const snn_status st = check_scan(cfg, T, B, F, plan);
     if (st != SNN_OK) return st;
     if (forward_bytes == nullptr || backward_bytes == nullptr) return SNN_E_NULL;
-    *forward_bytes = empty(T, B, F) ? 0 : size_t(scan_forward_workspace(cfg, T, B, F));
-    *backward_bytes = empty(T, B, F) ? 0 : size_t(scan_backward_workspace(cfg, T, B, F));
+    *forward_bytes = empty(T, B, F) ? 0 : size_t(scan_forward_workspace(cfg, plan, B, F));
+    *backward_bytes = empty(T, B, F) ? 0 : size_t(scan_backward_workspace(cfg, plan, T, B, F));
     return SNN_OK;
 }
 
@@ -198,13 +201,14 @@ snn_status snn_scan_forward(const snn_scan_cfg* cfg, int64_t T, int64_t B, int64
                             const snn_seq* dt, const float* A, const snn_seq* Bm, const snn_seq* Cm, const float* D,
                             const float* dt_bias, const float* h_in, const int32_t* lengths, const snn_seq* y,
                             float* h_out, void* saved, void* workspace, void* stream) {
-    snn_status st = check_scan(cfg, T, B, F);
+    ScanPlan plan;
+    snn_status st = check_scan(cfg, T, B, F, plan);
     if (st != SNN_OK || empty(T, B, F)) return st;
     st = first_error({check_scan_inputs(cfg, T, B, F, x, dt, A, Bm, Cm, D, dt_bias, h_in, lengths),
                       check_out(y, T, B, F, cfg->io), optional(h_out), optional(saved),
-                      check_workspace(workspace, scan_forward_workspace(cfg, T, B, F))});
+                      check_workspace(workspace, scan_forward_workspace(cfg, plan, B, F))});
     if (st != SNN_OK) return st;
-    ScanArgs a = scan_args(cfg, T, B, F, x, dt, A, Bm, Cm, D, dt_bias, h_in, lengths);
+    ScanArgs a = scan_args(cfg, plan, T, B, F, x, dt, A, Bm, Cm, D, dt_bias, h_in, lengths);
     a.y = rows(y);
     a.h_out = h_out;
     a.saved = static_cast<float*>(saved);
@@ -224,18 +228,19 @@ snn_status snn_scan_backward(const snn_scan_cfg* cfg, int64_t T, int64_t B, int6
                              const snn_seq* grad_y, const float* grad_h_out, const snn_seq* grad_x,
                              const snn_seq* grad_dt, float* grad_A, const snn_seq* grad_Bm, const snn_seq* grad_Cm,
                              float* grad_D, float* grad_dt_bias, float* grad_h_in, void* workspace, void* stream) {
-    snn_status st = check_scan(cfg, T, B, F);
+    ScanPlan plan;
+    snn_status st = check_scan(cfg, T, B, F, plan);
     if (st != SNN_OK || empty(T, B, F)) return st;
     const int io = cfg->io;
     const int64_t gs = int64_t(cfg->groups) * cfg->states;
     st = first_error({check_scan_inputs(cfg, T, B, F, x, dt, A, Bm, Cm, D, dt_bias, h_in, lengths),
-                      scan_saved(cfg, T, B, F) > 0 ? need(saved) : optional(saved), check_in(grad_y, T, B, F, io),
+                      scan_saved(cfg, plan, T, B, F) > 0 ? need(saved) : optional(saved), check_in(grad_y, T, B, F, io),
                       optional(grad_h_out), check_out(grad_x, T, B, F, io), check_out(grad_dt, T, B, F, io),
                       need(grad_A), check_out(grad_Bm, T, B, gs, io), check_out(grad_Cm, T, B, gs, io),
                       optional(grad_D), optional(grad_dt_bias), optional(grad_h_in),
-                      check_workspace(workspace, scan_backward_workspace(cfg, T, B, F))});
+                      check_workspace(workspace, scan_backward_workspace(cfg, plan, T, B, F))});
     if (st != SNN_OK) return st;
-    ScanArgs a = scan_args(cfg, T, B, F, x, dt, A, Bm, Cm, D, dt_bias, h_in, lengths);
+    ScanArgs a = scan_args(cfg, plan, T, B, F, x, dt, A, Bm, Cm, D, dt_bias, h_in, lengths);
     a.saved = static_cast<float*>(const_cast<void*>(saved));
     a.gy = rows(grad_y);
     a.gh_out = grad_h_out;

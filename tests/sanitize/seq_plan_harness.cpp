@@ -1,6 +1,8 @@
 // Host-only driver for AddressSanitizer / UndefinedBehaviorSanitizer runs, built with g++ (no GPU
 // code): what the sequence operators' plans (seq_host.h) decide, at the shapes that the GPU tests
 // use to reach a path.
+#include <chrono>
+#include <cmath>
 #include <cstdint>
 #include <cstdio>
 #include <initializer_list>
@@ -102,8 +104,39 @@ static void check_launches() {
     CHECK(layered_grid(ceil_div(int64_t(4096) * 1024 * 8 * 2 * 64, 1024), 1024).z > 1);
 }
 
+// 33 to 64 states: the segments' length is the cheapest of all multiples of 16 between half and twice
+// the one to start from, the shortest of several, and finding it does not take longer with more steps.
+static void check_segment_search() {
+    int searched = 0;
+    for (int64_t T : {128, 129, 333, 442, 1000, 4096, 20000})
+        for (int64_t B : {1, 2, 7})
+            for (int64_t F : {1, 64, 378, 1152, 2928, 4096})
+                for (int S : {33, 47, 64}) {
+                    const ScanPlan p = plan_of(T, B, F, S);
+                    if (p.segments == 1) continue;
+                    const int64_t groups = p.tiles * B, waves = groups * ceil_div(S, 4);
+                    const int64_t most = std::min({ceil_div(T, 16), int64_t(std::sqrt(2.0 * double(T))), kMaxSegments});
+                    const int64_t want = std::min(std::max<int64_t>(4096 / waves, 2), most);
+                    const auto cost = [&](int64_t n) { return ceil_div(groups * ceil_div(T, n), 256) * (n + 16); };
+                    const int64_t start = ceil_div(ceil_div(T, want), 16) * 16;
+                    int64_t best = start;
+                    for (int64_t n = 16; n < T; n += 16)
+                        if (n >= start / 32 * 16 && n <= 2 * start && ceil_div(T, n) <= most && cost(n) < cost(best)) best = n;
+                    CHECK(p.steps == best);
+                    searched += best != start;
+                }
+    CHECK(searched > 10);
+    const auto from = std::chrono::steady_clock::now();
+    int64_t sum = 0;
+    for (int i = 0; i < 400; ++i) sum += plan_of((1 << 24) + i, 1, 2928, 64).segments;
+    CHECK(sum > 400);
+    // a search through all lengths takes 3 ms each, and more under the sanitizers
+    CHECK(std::chrono::duration<double>(std::chrono::steady_clock::now() - from).count() < 0.4);
+}
+
 int main() {
     check_states_in_place();
+    check_segment_search();
     check_launches();
     if (failures != 0) return 1;
     std::puts("all checks passed");
