@@ -134,8 +134,30 @@ static void check_segment_search() {
     CHECK(std::chrono::duration<double>(std::chrono::steady_clock::now() - from).count() < 0.4);
 }
 
+// The shapes of tests/test_gpu_sequence_long.py.
+static void check_paths() {
+    CHECK(plan_of(4096, 1, 20, 16).segments > kWalkSegments);
+    CHECK(plan_of(3300, 3, 6, 3, 2).segments > kWalkSegments);
+    CHECK(plan_of(3200, 2, 40, 33).segments > kWalkSegments);
+    const ScanPlan rounds = plan_of(160, 2, 2928, 47);
+    CHECK(rounds.waves == 16 && rounds.segments > 1 && rounds.tiles * 2 * rounds.segments > 256);
+    struct Conv {
+        int io, width;
+        int64_t T, B, F;
+    };
+    for (const Conv& s : {Conv{SNN_IO_BF16, 4, 1003, 16, 2059}, {SNN_IO_F32, 3, 700, 9, 2051}, {SNN_IO_BF16, 8, 2100, 8, 2056}})
+        for (bool backward : {false, true}) {
+            const snn_conv_cfg c = {s.io, s.width, SNN_ACT_SILU};
+            const ConvPlan p = conv_plan(&c, s.T, s.B, s.F, backward);
+            CHECK(p.steps > conv_rows(backward) && p.chunks > 1);
+        }
+    for (const auto& [T, B, F] : {std::tuple<int64_t, int64_t, int64_t>{250, 5, 4097}, {1100, 4, 1030}, {130, 5, 9000}, {3000, 3, 66}})
+        for (bool backward : {false, true}) CHECK(norm_groups(T, B, F, backward) < T * B);
+}
+
 int main() {
     check_states_in_place();
+    check_paths();
     check_segment_search();
     check_launches();
     if (failures != 0) return 1;
