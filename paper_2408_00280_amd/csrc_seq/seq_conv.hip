@@ -225,10 +225,11 @@ __device__ void conv_backward_walk(const ConvArgs& a, const ConvLane& l) {
                 for (int i = 0; i < W; ++i) u = fmaf(w[j][i], hist[i][j], u);
                 g[j] = IoVec<IO, V>::get(gy, j);
                 if (ACT == SNN_ACT_SILU) g[j] *= silu_slope(u, sigmoid(u));
-                const float own = inner.value || t < stop ? g[j] : 0.0f;   // steps past the chunk are another's
-                gb[j] += own;
+                if (inner.value || t < stop) {       // steps past the chunk are another's
+                    gb[j] += g[j];
 #pragma unroll
-                for (int i = 0; i < W; ++i) gw[j][i] = fmaf(own, hist[i][j], gw[j][i]);
+                    for (int i = 0; i < W; ++i) gw[j][i] = fmaf(g[j], hist[i][j], gw[j][i]);
+                }
 #pragma unroll
                 for (int i = 0; i < W - 1; ++i) hist[i][j] = hist[i + 1][j];
             }

@@ -87,3 +87,20 @@ def test_infinite_b_and_c(ops, which, T, S):
     for name, v in {"y": y, "h_out": h, **{k: got[k] for k in ("gx", "gdt", "gA", "gB", "gC")}}.items():
         assert torch.equal(torch.isinf(v.cpu()), torch.isinf(ref[name])), name
         assert torch.equal(torch.isnan(v.cpu()), torch.isnan(ref[name])), name
+
+
+@pytest.mark.parametrize("io,F", [("f32", 9), ("bf16", 64)])
+@pytest.mark.parametrize("at", [0, 7, 8, 9, 10, 11, 39])
+def test_infinite_inputs_of_a_convolution(ops, at, io, F):
+    """An infinite input gives its own filter infinite gradients, wherever it lies to the chunks that
+    share out the steps, and no others."""
+    T, B, W = 40, 2, 4
+    dt = {"f32": torch.float32, "bf16": torch.bfloat16}[io]
+    x, gy = positive(1, T, B, F).to(dt), positive(2, T, B, F).to(dt)
+    w, bias = normal(3, F, W), normal(4, F)
+    x[at, 1, F - 2] = float("inf")
+    gx, gw, gb, _ = ops.conv_backward(x, w, bias, gy, act=None)
+    ref = R.conv(x, w, bias, act=None, gy=gy)
+    for name, v in (("gx", gx), ("gw", gw), ("gb", gb)):
+        assert torch.equal(torch.isinf(v.cpu()), torch.isinf(ref[name])), name
+        assert torch.equal(torch.isnan(v.cpu()), torch.isnan(ref[name])), name
