@@ -10,8 +10,10 @@ what lies behind is not read, and is 0 in outputs and gradients.
 
 Checks, outputs and workspaces are made in csrc_seq/seq_torch.cpp, which calls the C ABI; wrong
 arguments raise ValueError, refused ones native.SnnError.  Torch provides device memory and
-streams only.  Work is enqueued on torch's current stream
-of the tensors' device, or on ``stream`` (a torch.cuda.Stream or a raw handle).
+streams only.  Work is enqueued on torch's current stream of the tensors' device, or on ``stream``
+(a torch.cuda.Stream of that device or a raw handle): then the order of the two streams is the
+caller's.  Memory of tensors that are dropped meanwhile is kept until a torch.cuda.Stream is done
+with it; behind a raw handle, whose life torch does not know, the caller keeps them.
 """
 from __future__ import annotations
 
@@ -36,6 +38,10 @@ def act_code(act) -> int:
     return ACTS[act]
 
 
+def _tensors(values):
+    return [v for v in values if isinstance(v, torch.Tensor) and v.is_cuda]
+
+
 def _on_stream(fn):
     """fn on `stream`, which belongs to its first tensor's device."""
     first = fn.__code__.co_varnames[0]
@@ -47,11 +53,22 @@ def _on_stream(fn):
         x = args[0] if args else kw[first]
         if not x.is_cuda:
             raise ValueError("tensors must be on the GPU")
+        known = isinstance(stream, torch.cuda.Stream)
+        if known and stream.device != x.device:
+            raise ValueError(f"stream is one of {stream.device}, the tensors are on {x.device}")
         with torch.cuda.device(x.device):
-            if not isinstance(stream, torch.cuda.Stream):
+            if not known:
                 stream = torch.cuda.ExternalStream(int(stream)) if stream else torch.cuda.default_stream()
+            current = torch.cuda.current_stream()
             with torch.cuda.stream(stream):
-                return fn(*args, **kw)
+                out = fn(*args, **kw)
+            if known and stream != current:
+                # neither side's memory goes to another tensor while the other side may be using it
+                for t in _tensors([*args, *kw.values()]):
+                    t.record_stream(stream)
+                for t in _tensors(out if isinstance(out, tuple) else [out]):
+                    t.record_stream(current)
+            return out
     return call
 
 

@@ -127,3 +127,31 @@ def test_windows_that_overlap(ops, steps):
 
 def positive_rates(F, S):
     return normal(2, F, S).abs() + 0.1
+
+
+def test_tensors_dropped_while_another_stream_uses_them(ops):
+    """Inputs dropped behind a call on another stream, and outputs dropped behind their use on this
+    one, keep their memory until the other side has come to it."""
+    T, B, F = 64, 8, 4100
+    w, stream = normal(2, F, 4), torch.cuda.Stream()
+    x = normal(1, T, B, F)
+    want = ops.conv_forward(x, w)
+    ref = want.clone()
+    torch.cuda.synchronize()
+    with torch.cuda.stream(stream):
+        torch.cuda._sleep(20_000_000)                       # some 10 ms
+    y = ops.conv_forward(x, w, stream=stream)
+    at = x.data_ptr()
+    del x
+    others = [torch.zeros(T, B, F, device="cuda") for _ in range(3)]
+    assert all(v.data_ptr() != at for v in others)
+    torch.cuda.synchronize()
+    assert torch.equal(y, ref)
+    torch.cuda._sleep(20_000_000)
+    kept, at = y + 1, y.data_ptr()
+    del y
+    with torch.cuda.stream(stream):
+        others = [torch.zeros(T, B, F, device="cuda") for _ in range(3)]
+    assert all(v.data_ptr() != at for v in others)
+    torch.cuda.synchronize()
+    assert torch.equal(kept, ref + 1)
