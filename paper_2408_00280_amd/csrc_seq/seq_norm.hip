@@ -208,7 +208,8 @@ __global__ __launch_bounds__(MAXT) void norm_backward_kernel(NormArgs a) {
     lane.params(a.scale, 1.0f, scale);
     lane.params(a.w_pre, 0.0f, w_pre);
     // 16 waves of one workgroup have no registers for the next row's loads and the sums: those
-    // are in LDS then, each lane's own (x[1024][8][8192] bf16: 289 us, 383 with spilled registers)
+    // are in LDS then, each lane's own, and some 90 registers are spilled all the same
+    // (x[1024][8][8192] bf16: 290 us, 383 with the sums and loads among them)
     constexpr bool kAhead = MAXT < 1024;
     __shared__ f32x4_t sums[kAhead ? 1 : 6][kAhead ? 1 : MAXT];
     const auto open = [&](int k, float (&g)[kNormLane]) {
@@ -543,7 +544,8 @@ __global__ __launch_bounds__(1024) void reduce_kernel(const float* part, int64_t
 snn_status reduce_entry(const float* part, int64_t P, int64_t stride, const ReduceOut& out, hipStream_t s) {
     const int64_t n = out.n[0] + out.n[1] + out.n[2];
     // Many partial results of few values: 16 values per workgroup, so that more CUs read them
-    // (2924 of 405 values: 9 us to 14; 4096 of 1536: 13 to 15; of 4080 the other way, 10 to 9).
+    // (4096 of 120 values: 9 us to 16; of 405, 11 to 18; 3200 of 1536, 11 to 12; 2048 of 2040, 9 to
+    // 10; 4096 of 4080 the other way, 10 to 9).
     if (P >= 256 && n <= 32 * kWave) return launch_blk(reduce_kernel<16>, grid_for(n, 16), 1024, s, part, P, stride, out);
     const int waves = P >= 16 ? 16 : P >= 4 ? 4 : 1;
     return launch_blk(reduce_kernel<kWave>, grid_for(n, kWave), waves * kWave, s, part, P, stride, out);
