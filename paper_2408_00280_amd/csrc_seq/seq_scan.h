@@ -16,7 +16,7 @@ struct ScanPlace {
     int t0, t1, len;     // the segment, and the steps of the sequence
 };
 
-// The workgroup's number; false behind the last.
+// The workgroup's number, and whether it has work: a grid of several layers ends with some that have none.
 __device__ __forceinline__ unsigned scan_block(const ScanArgs& a) { return blockIdx.z * a.layer + blockIdx.x; }
 __device__ __forceinline__ bool scan_has_block(const ScanArgs& a) {
     return scan_block(a) < unsigned(a.plan.tiles) * unsigned(a.G) * unsigned(a.B);

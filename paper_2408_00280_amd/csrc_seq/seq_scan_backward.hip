@@ -44,7 +44,8 @@ struct __align__(16) Step {
 
 // Adds one block's part of dL/dA, the first of those that a workgroup goes through, up to the
 // sequence's last step: from memory, each step's state from the block's start.  Hardly a call
-// needs it, so that it takes the kernel's arguments anew rather than hold registers until then.
+// needs it, so that it takes the kernel's arguments anew (a ScanArgs is all of them) rather than
+// hold registers until then.
 template <int IO, int K>
 __device__ void add_block_rates(int t0, float (&gA)[kSL]) {
     auto args = __builtin_amdgcn_kernarg_segment_ptr();
@@ -309,8 +310,8 @@ __global__ __launch_bounds__(NS * kWave, backward_waves(NS)) void scan_backward_
         lds_barrier();
         buf ^= 1;
     }
-    if (a.gh_in != nullptr && p.t0 == 0) store_state(a, p, a.gh_in, e);
     if (again >= 0) add_block_rates<IO, K>(again, gA);
+    if (a.gh_in != nullptr && p.t0 == 0) store_state(a, p, a.gh_in, e);
     float* pf = a.part_f + (blockIdx.y * a.B + p.b) * scan_partial_values(a.F, a.S);
 #pragma unroll
     for (int i = 0; i < kSL; ++i)

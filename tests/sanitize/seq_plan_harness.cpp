@@ -33,7 +33,7 @@ static void check_states_in_place() {
     float states[2] = {};
     float *h = &states[0], *other = &states[1];
     bool several = false, many = false;
-    for (int64_t T : {1, 2, 127, 128, 270, 333, 442, 3072, 4096, 131072})
+    for (int64_t T : {1, 2, 127, 128, 270, 333, 442, 3300, 4096, 131072})
         for (int64_t B : {1, 2, 7})
             for (int64_t F : {1, 64, 777, 2928})
                 for (int S : {1, 7, 16, 47, 64}) {
