@@ -90,14 +90,13 @@ struct StateColumn {
     }
 };
 
-// 2^x h over a segment, x the sum of its steps times the rate.  The decays of a whole segment may
-// multiply to 0 or to infinity in 32 bits where no step's does.  By the whole part of x first, a
-// state that is 0 stays 0 and one that is not finite stays so, as they do step by step, and any
-// other leaves the type only where the product does (2^+-512 takes all of them out of it).
-__device__ __forceinline__ float decayed(float x, float h) {
-    x = __builtin_amdgcn_fmed3f(x, -512.0f, 512.0f);
-    const float whole = floorf(x);
-    return ldexpf(h, int(whole)) * __builtin_amdgcn_exp2f(x - whole);
+// 2^x h over a segment, of half x, the sum of its steps times the rate.  The decays of a whole
+// segment may multiply to 0 or to infinity in 32 bits where no step's does.  As the root twice, kept
+// finite and above 0, they leave a state that is 0 or not finite as it is, as step by step, and
+// take any other out of the type only where their product does.
+__device__ __forceinline__ float decayed(float half, float h) {
+    const float root = __builtin_amdgcn_fmed3f(__builtin_amdgcn_exp2f(half), __FLT_MIN__, __FLT_MAX__);
+    return h * root * root;
 }
 
 // The state before this segment, or e behind it (DOWN): the workgroup walks the others' states and
@@ -131,7 +130,7 @@ __device__ __forceinline__ void segment_state(const ScanArgs& a, const ScanPlace
         for (int u = 0; u < U; ++u) {
             if (c0 + u < n) {
 #pragma unroll
-                for (int s = 0; s < kSL; ++s) h[s] = decayed(d[u] * rate[s], h[s]) + l[u][s];
+                for (int s = 0; s < kSL; ++s) h[s] = decayed(0.5f * d[u] * rate[s], h[s]) + l[u][s];
             }
         }
     }

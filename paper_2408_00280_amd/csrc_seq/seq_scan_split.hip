@@ -145,7 +145,7 @@ __global__ __launch_bounds__(kBlock) void scan_carry_kernel(ScanArgs a, int64_t 
         for (int u = 0; u < U; ++u) {
             if (c0 + u < a.plan.segments) {
                 a.part_h[(DOWN ? a.plan.segments - 1 - c0 - u : c0 + u) * n + i] = h;
-                if (c0 + u + 1 < a.plan.segments) h = decayed(d[u] * rate, h) + local[u];
+                if (c0 + u + 1 < a.plan.segments) h = decayed(0.5f * d[u] * rate, h) + local[u];
             }
         }
     }
